@@ -10,7 +10,8 @@ Kinds of cases
 
 Tensors are NHWC bf16 with a channel pitch that is a multiple of 16, as the convolutions read and write them; parameters and
 statistics are fp32. A checkpoint holds one int8 code per value and one byte per block of 32 consecutive channels of a pixel: the
-block's scale is 2^(byte - 127), the smallest power of two that brings its values into [-127, 127]. Byte 255: the block stands for NaN.
+block's scale is 2^(byte - 127), the smallest power of two, of 2^-127 .. 2^121, that brings its values into [-127, 127]. Byte 255: the block
+stands for NaN.
 """
 import math
 
@@ -101,10 +102,10 @@ def _quantise(x):
     amax = f.abs().amax(-1)
     bad = ~torch.isfinite(f).all(-1)
     m, k = torch.frexp(torch.where(bad, torch.zeros_like(amax), amax))   # amax = m * 2^k, m in [0.5, 1): m * 128 rounds to 128 from 127.5 on
-    e = torch.where(m * 128 >= 127.5, k - 6, k - 7).clamp_(min=-127)
+    e = torch.where(m * 128 >= 127.5, k - 6, k - 7).clamp_(min=-127, max=121)
     e = torch.where(amax == 0, torch.full_like(e, -127), e)
     # (2^-e in two factors: one alone may be too large for fp32)
-    q = torch.ldexp(torch.ldexp(f, (-e // 2).unsqueeze(-1)), (-e - (-e // 2)).unsqueeze(-1)).round_()
+    q = torch.ldexp(torch.ldexp(f, (-e // 2).unsqueeze(-1)), (-e - (-e // 2)).unsqueeze(-1)).round_().clamp_(min=-127, max=127)
     q = torch.where(bad.unsqueeze(-1), torch.zeros_like(q), q)
     return q.flatten(-2)[..., :C].to(torch.int8), torch.where(bad, torch.full_like(e, 255), e + 127).to(torch.uint8)
 
@@ -329,8 +330,8 @@ def exact(case, seed):
             blk = v[..., b:b + 32]
             top = blk.abs().amax(-1, keepdim=True)
             step = torch.exp2(torch.ceil(torch.log2(top.clamp(min=1e-300) / 127)))
-            step = torch.where(torch.round(top / (step / 2)) <= 127, step / 2, step).clamp(min=2.0 ** -127)
-            out[..., b:b + 32] = torch.round(blk / step) * step
+            step = torch.where(torch.round(top / (step / 2)) <= 127, step / 2, step).clamp(min=2.0 ** -127, max=2.0 ** 121)
+            out[..., b:b + 32] = torch.round(blk / step).clamp(min=-127, max=127) * step
         return out
 
     if kind == "checkpoint":
