@@ -255,6 +255,78 @@ pt_status pt_bn_relu_bwd(pt_ctx *ctx, const pt_bn_desc *d, const void *x, const 
                          float *dbeta, void *ws, size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Group normalisation (no counterpart in the paper, whose networks use batch normalisation: for mini-batches too small for batch
+ * statistics, per GPU or altogether) with the residual add of a block and an activation fused in, channels last. Activations are NHWC
+ * bf16 with channel pitch ld as above. The C channels form `groups` groups of consecutive channels; per image n and group g of
+ * m = H*W*|g| values:
+ *     mean = sum(x)/m, var = sum((x-mean)^2)/m, rstd = 1/sqrt(var+eps), xhat = (x-mean)*rstd, z = gamma*xhat + beta (+ residual),
+ *     y = act(z):  PT_ACT_NONE z,  PT_ACT_RELU max(z, 0),  PT_ACT_SILU z/(1+exp(-z)).
+ * Backward, with the given mean and rstd:
+ *     dz = dy*act'(z) (PT_ACT_RELU: dy where z > 0, decided in 64 bits, else 0), dbeta = sum(dz), dgamma = sum(dz*xhat) over the images,
+ *     A = sum(gamma*dz)/m, B = sum(gamma*dz*xhat)/m over the group, dx = rstd*(gamma*dz - A - xhat*B), dresidual = dz.
+ * All pointers are device pointers but group_begin. x, residual, y, dy, dx, dresidual are 16-byte aligned [N][H][W][ld] bf16 tensors whose
+ * pad lanes are never used and are written as zeros in the outputs; gamma, beta and their gradients are fp32 vectors of C elements,
+ * save_mean and save_rstd fp32 [N][groups]. Sums are combined in a fixed order (run-to-run identical). An output may be the same tensor
+ * as an input of its call (y as x or residual; dx and dresidual as x, residual or dy, but not as each other); otherwise no two overlap.
+ * An infinity or a NaN in x makes the outputs of its image and group NaN.
+ * The current device must be the context's. PT_ERR_INVALID_ARG for bad sizes, pitches, alignment, groups, missing pointers or another
+ * current device; PT_ERR_UNSUPPORTED for ld > 2048, H*W >= 2^31, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.
+ * ------------------------------------------------------------------------------------------ */
+enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_SILU = 2 };
+typedef struct {
+    int32_t N, H, W, C;
+    int32_t ld;        /* channel pitch (elements, multiple of 8, >= C, <= 2048) */
+    int32_t ldq;       /* pitch of a checkpoint's codes (bytes, multiple of 8, >= C); read by calls that take a checkpoint */
+    int32_t groups;    /* 1 .. C; C must be a multiple of it unless group_begin is given */
+    int32_t act;       /* PT_ACT_* */
+    float eps;         /* >= 0 */
+    const int32_t *group_begin;   /* host, optional: groups + 1 ascending channel indices, the first 0, the last C; group g is the channels
+                                     [group_begin[g], group_begin[g + 1]). What pruning leaves of a layer's groups is not of equal sizes.
+                                     Read during the call only. */
+} pt_gn_desc;
+
+/* The checkpoint of an activation tensor: 8 bits per value, for what the backward pass needs of a forward pass. codes: int8
+ * [npix][ldq]; scales: uint8 [npix][ceil(C/32)] dense, both 16-byte aligned. A block is 32 consecutive channels of a pixel (the last one
+ * of a pixel may be shorter); with amax its largest |x|,
+ *     e = the smallest integer in [-127, 121] with rint(amax / 2^e) <= 127 (121 if there is none: the largest bf16 is 127.5 * 2^121),
+ *     code = rint(x / 2^e) (ties to even) within [-127, 127],  scale byte = e + 127,
+ * and a value is restored as code * 2^e, exactly representable in bf16: off by at most amax/127 of the block (2^-128 in a block of
+ * subnormal size). A block that holds an
+ * infinity or a NaN gets scale byte 255 and codes 0 and is restored as NaN. Codes of the channels C .. up to the next multiple of 8 are
+ * written as zeros; beyond that codes are left untouched. */
+typedef struct {
+    int64_t npix;      /* pixels: N*H*W, >= 0 */
+    int32_t C, ld;     /* channels, pitch of the bf16 tensor (elements, multiple of 8, >= C, <= 2048) */
+    int32_t ldq;       /* pitch of the codes (bytes, multiple of 8, >= C) */
+} pt_pack_desc;
+/* Bytes to allocate for the scales of a checkpoint: npix * ceil(C/32), rounded up to a multiple of 16 (0 for invalid arguments). */
+size_t pt_act_scale_bytes(int64_t npix, int32_t C);
+/* x (bf16 [npix][ld]) into a checkpoint, and a checkpoint into x (pad lanes written as zeros). PT_ERR_INVALID_ARG for bad sizes,
+ * pitches, alignment, null pointers or a current device other than the context's; PT_ERR_UNSUPPORTED for ld > 2048. */
+pt_status pt_act_pack(pt_ctx *ctx, const pt_pack_desc *d, const void *x, void *codes, void *scales, void *stream);
+pt_status pt_act_unpack(pt_ctx *ctx, const pt_pack_desc *d, const void *codes, const void *scales, void *x, void *stream);
+
+/* Bytes of workspace the two backward calls need for this descriptor (0 if it is invalid). */
+size_t pt_gn_workspace_bytes(const pt_ctx *ctx, const pt_gn_desc *d);
+
+/* y = act(gamma*xhat + beta + residual). residual may be NULL. save_mean, save_rstd receive what the backward pass needs. codes and
+ * scales: both NULL, or the checkpoint of x (as pt_act_pack leaves it, with npix = N*H*W), taken on the way. */
+pt_status pt_gn_act_fwd(pt_ctx *ctx, const pt_gn_desc *d, const void *x, const void *residual, const float *gamma, const float *beta,
+                        float *save_mean, float *save_rstd, void *y, void *codes, void *scales, void *stream);
+
+/* Gradients of the call above. residual as in the forward pass; dresidual may be NULL. */
+pt_status pt_gn_act_bwd(pt_ctx *ctx, const pt_gn_desc *d, const void *x, const void *residual, const void *dy, const float *gamma,
+                        const float *beta, const float *save_mean, const float *save_rstd, void *dx, void *dresidual, float *dgamma,
+                        float *dbeta, void *ws, size_t ws_bytes, void *stream);
+
+/* The same from the checkpoint of x: the gradients pt_gn_act_bwd gives for the restored tensor (the statistics are those of the forward
+ * pass, taken from x itself). y (optional) receives act(z) of the restored x: the input of the convolution that follows, for its weight
+ * gradient, so that a layer has to keep its checkpoint and nothing else. */
+pt_status pt_gn_act_bwd_packed(pt_ctx *ctx, const pt_gn_desc *d, const void *codes, const void *scales, const void *residual,
+                               const void *dy, const float *gamma, const float *beta, const float *save_mean, const float *save_rstd, void *dx,
+                               void *dresidual, float *dgamma, float *dbeta, void *y, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Max pooling (Sec. 2.1 counts the pooling layers among the cheap, bandwidth-bound layers; ResNet has one, after its first
  * convolution). Present so that a training step can be chained from the image to the last feature map. Activations as above:
  * [N][H][W][ld] bf16, 16-byte aligned, ld a multiple of 8; square window R, stride, padding pad < R; output

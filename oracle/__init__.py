@@ -353,6 +353,100 @@ def bn_relu_bwd(x, y, dy, gamma, mean, invstd, relu: bool = True):
     return dx, dz, dgamma, dbeta
 
 
+# ------------------------------------------------------------------------------------------------------------ group normalisation
+def group_begin(C: int, groups: int) -> List[int]:
+    """First channel of each of `groups` groups, and C: equal groups where C is a multiple, else as equal as whole channels allow."""
+    return [g * C // groups for g in range(groups + 1)]
+
+
+def _act(z, act: int):
+    """0: identity, 1: ReLU (a NaN stays a NaN), 2: z * sigmoid(z)."""
+    if act == 1:
+        return np.where(z > 0, z, np.where(np.isnan(z), z, 0.0))
+    return z / (1.0 + np.exp(-z)) if act == 2 else z
+
+
+def gn_act_fwd(x, gamma, beta, begin: Sequence[int], eps: float = 1e-5, residual=None, act: int = 1):
+    """Group normalisation of x [N][H][W][C] with a residual add and an activation. Per image and group of channels
+    [begin[g], begin[g + 1]): mean and biased variance over its positions and channels,
+        xhat = (x - mean) / sqrt(var + eps),  z = gamma*xhat + beta (+ residual),  y = act(z).
+    Returns y, mean [N][G], rstd [N][G], all fp64."""
+    x = np.asarray(x, np.float64)
+    y = np.empty_like(x)
+    N, G = x.shape[0], len(begin) - 1
+    mean, rstd = np.empty((N, G)), np.empty((N, G))
+    for n in range(N):
+        for g in range(G):
+            c = slice(begin[g], begin[g + 1])
+            v = x[n, ..., c]
+            mean[n, g] = v.sum() / v.size
+            rstd[n, g] = 1.0 / np.sqrt(((v - mean[n, g]) ** 2).sum() / v.size + eps)
+            z = (v - mean[n, g]) * rstd[n, g] * np.asarray(gamma, np.float64)[c] + np.asarray(beta, np.float64)[c]
+            if residual is not None:
+                z = z + np.asarray(residual, np.float64)[n, ..., c]
+            y[n, ..., c] = _act(z, act)
+    return y, mean, rstd
+
+
+def gn_act_bwd(x, dy, gamma, beta, mean, rstd, begin: Sequence[int], residual=None, act: int = 1):
+    """Back-propagation through gn_act_fwd with the given statistics. dz = dy * act'(z) (ReLU: dy where z > 0);
+        dbeta = sum(dz), dgamma = sum(dz*xhat), dresidual = dz,
+        dx = rstd * (gamma*dz - A - xhat*B), A and B the means of gamma*dz and gamma*dz*xhat over the image's group.
+    Returns dx, dresidual, dgamma, dbeta, y = act(z) (fp64)."""
+    x, dy = np.asarray(x, np.float64), np.asarray(dy, np.float64)
+    gamma, beta = np.asarray(gamma, np.float64), np.asarray(beta, np.float64)
+    dx, dz, y = np.empty_like(x), np.empty_like(x), np.empty_like(x)
+    dgamma, dbeta = np.zeros(x.shape[-1]), np.zeros(x.shape[-1])
+    for n in range(x.shape[0]):
+        for g in range(len(begin) - 1):
+            c = slice(begin[g], begin[g + 1])
+            xhat = (x[n, ..., c] - float(mean[n, g])) * float(rstd[n, g])
+            z = xhat * gamma[c] + beta[c]
+            if residual is not None:
+                z = z + np.asarray(residual, np.float64)[n, ..., c]
+            y[n, ..., c] = _act(z, act)
+            d = dy[n, ..., c]
+            if act == 1:
+                d = np.where(z > 0, d, 0.0)
+            elif act == 2:
+                s = 1.0 / (1.0 + np.exp(-z))
+                d = d * (s + z * s * (1.0 - s))
+            dbeta[c] += d.sum((0, 1))
+            dgamma[c] += (d * xhat).sum((0, 1))
+            w = d * gamma[c]
+            dx[n, ..., c] = float(rstd[n, g]) * (w - w.mean() - xhat * (w * xhat).mean())
+            dz[n, ..., c] = d
+    return dx, dz, dgamma, dbeta, y
+
+
+def act_pack(x):
+    """The 8-bit checkpoint of x [..., C]: blocks of 32 consecutive channels; e is the smallest integer in [-127, 121] for
+    which every rint(x / 2^e) (ties to even) of the block lies within [-127, 127], 121 if there is none (the largest bf16 is
+    127.5 * 2^121); code = rint(x / 2^e) within [-127, 127], scale byte e + 127. A block with an infinity or a NaN: scale byte 255, codes 0. Returns codes int8 [..., C], scale bytes uint8 [..., ceil(C / 32)]."""
+    x = np.asarray(x, np.float64)
+    C = x.shape[-1]
+    codes, scales = np.zeros(x.shape, np.int8), np.zeros(x.shape[:-1] + ((C + 31) // 32,), np.uint8)
+    for at in np.ndindex(x.shape[:-1]):
+        for b in range(0, C, 32):
+            v = x[at][b:b + 32]
+            if not np.all(np.isfinite(v)):
+                scales[at][b // 32] = 255
+                continue
+            e = -127
+            while e < 121 and np.abs(np.rint(np.ldexp(v, -e))).max() > 127:
+                e += 1
+            scales[at][b // 32] = e + 127
+            codes[at][b:b + 32] = np.clip(np.rint(np.ldexp(v, -e)), -127, 127).astype(np.int8)
+    return codes, scales
+
+
+def act_unpack(codes, scales) -> np.ndarray:
+    """The values a checkpoint stands for: code * 2^(scale byte - 127), NaN where the scale byte is 255 (fp64)."""
+    s = np.repeat(np.asarray(scales).astype(np.int64), 32, axis=-1)[..., :np.shape(codes)[-1]]
+    v = np.ldexp(np.asarray(codes, np.float64), s - 127)
+    return np.where(s == 255, np.nan, v)
+
+
 # --------------------------------------------------------------------------- pooling (Sec. 2.1)
 def maxpool_fwd(x, R: int = 3, stride: int = 2, pad: int = 1):
     """Max pooling of x [N][H][W][C] (Sec. 2.1 lists pooling among the layers of a CNN; ResNet pools once, after its first

@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpt_b200.so")
 
 PT_OK = 0
+PT_ACT_NONE, PT_ACT_RELU, PT_ACT_SILU = 0, 1, 2
 PT_CONV_FWD, PT_CONV_DGRAD, PT_CONV_WGRAD = 0, 1, 2
 PT_FORM_ANY, PT_FORM_WGRAD_PIXELS, PT_FORM_WGRAD_ROWS, PT_FORM_WGRAD_TAPS, PT_FORM_WGRAD_PACKED = 0, 1, 2, 3, 4
 PT_FORM_GEMM, PT_FORM_HALO, PT_FORM_PLANES, PT_FORM_STEM = 5, 6, 7, 8
@@ -52,6 +53,15 @@ class pt_sgd_hparams(Structure):
 class pt_bn_desc(Structure):
     _fields_ = [("N", c_int32), ("H", c_int32), ("W", c_int32), ("C", c_int32), ("ld", c_int32),
                 ("eps", c_float), ("momentum", c_float), ("relu", c_int32)]
+
+
+class pt_gn_desc(Structure):
+    _fields_ = [(n, c_int32) for n in ("N", "H", "W", "C", "ld", "ldq", "groups", "act")] + [("eps", c_float),
+                                                                                            ("group_begin", POINTER(c_int32))]
+
+
+class pt_pack_desc(Structure):
+    _fields_ = [("npix", c_int64), ("C", c_int32), ("ld", c_int32), ("ldq", c_int32)]
 
 
 class pt_pool_desc(Structure):
@@ -115,6 +125,13 @@ EXPORTS = {
     "pt_bn_workspace_bytes": (c_size_t, [c_void_p, POINTER(pt_bn_desc)]),
     "pt_bn_relu_fwd": (c_int32, [c_void_p, POINTER(pt_bn_desc)] + [c_void_p] * 9 + [c_void_p, c_size_t, c_void_p]),
     "pt_bn_relu_bwd": (c_int32, [c_void_p, POINTER(pt_bn_desc)] + [c_void_p] * 10 + [c_void_p, c_size_t, c_void_p]),
+    "pt_gn_workspace_bytes": (c_size_t, [c_void_p, POINTER(pt_gn_desc)]),
+    "pt_gn_act_fwd": (c_int32, [c_void_p, POINTER(pt_gn_desc)] + [c_void_p] * 10),
+    "pt_gn_act_bwd": (c_int32, [c_void_p, POINTER(pt_gn_desc)] + [c_void_p] * 12 + [c_size_t, c_void_p]),
+    "pt_gn_act_bwd_packed": (c_int32, [c_void_p, POINTER(pt_gn_desc)] + [c_void_p] * 14 + [c_size_t, c_void_p]),
+    "pt_act_scale_bytes": (c_size_t, [c_int64, c_int32]),
+    "pt_act_pack": (c_int32, [c_void_p, POINTER(pt_pack_desc)] + [c_void_p] * 4),
+    "pt_act_unpack": (c_int32, [c_void_p, POINTER(pt_pack_desc)] + [c_void_p] * 4),
     "pt_training_memory_bytes": (c_size_t, [POINTER(pt_layer_shape), c_int32, c_int32]),
     "pt_update_mini_batch": (c_int32, [POINTER(pt_layer_shape), c_int32, c_size_t, c_int32, c_float, c_int32, POINTER(c_int32), POINTER(c_float)]),
     "pt_cross_entropy_workspace_bytes": (c_size_t, [c_int32]),
@@ -373,6 +390,65 @@ def pt_bn_relu_bwd(ctx, d, x, y, dy, gamma, save_mean, save_invstd, dx, dresidua
     p, n = _ws(ws)
     _check(lib().pt_bn_relu_bwd(ctx.handle, byref(d), _ptr(x), _ptr(y), _ptr(dy), _ptr(gamma), _ptr(save_mean), _ptr(save_invstd),
                                 _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), p, n, _stream(stream)), "pt_bn_relu_bwd")
+
+
+def make_gn_desc(N, H, W, C, groups, ld=None, eps=1e-5, act=PT_ACT_RELU, group_begin=None, ldq=None) -> pt_gn_desc:
+    """group_begin: the groups' first channels, and C (groups + 1 numbers); None: equal groups."""
+    p8 = (C + 7) // 8 * 8
+    if group_begin is not None:
+        group_begin = [int(b) for b in group_begin]
+        if len(group_begin) != groups + 1:
+            raise ValueError(f"group_begin has {len(group_begin)} entries for {groups} groups: groups + 1 are wanted")
+        group_begin = (c_int32 * len(group_begin))(*group_begin)       # (the descriptor's pointer keeps it alive)
+    return pt_gn_desc(N, H, W, C, ld or p8, ldq or p8, groups, act, eps, group_begin)
+
+
+def pt_gn_workspace_bytes(ctx, d: pt_gn_desc) -> int:
+    return int(lib().pt_gn_workspace_bytes(ctx.handle, byref(d)))
+
+
+def pt_gn_act_fwd(ctx, d, x, residual, gamma, beta, save_mean, save_rstd, y, codes=None, scales=None, stream=None):
+    _check(lib().pt_gn_act_fwd(ctx.handle, byref(d), _ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), _ptr(save_mean), _ptr(save_rstd),
+                               _ptr(y), _ptr(codes), _ptr(scales), _stream(stream)), "pt_gn_act_fwd")
+
+
+def pt_gn_act_bwd(ctx, d, x, residual, dy, gamma, beta, save_mean, save_rstd, dx, dresidual, dgamma, dbeta, ws, stream=None):
+    p, n = _ws(ws)
+    _check(lib().pt_gn_act_bwd(ctx.handle, byref(d), _ptr(x), _ptr(residual), _ptr(dy), _ptr(gamma), _ptr(beta), _ptr(save_mean),
+                               _ptr(save_rstd), _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), p, n, _stream(stream)),
+           "pt_gn_act_bwd")
+
+
+def pt_gn_act_bwd_packed(ctx, d, codes, scales, residual, dy, gamma, beta, save_mean, save_rstd, dx, dresidual, dgamma, dbeta, y, ws,
+                         stream=None):
+    p, n = _ws(ws)
+    _check(lib().pt_gn_act_bwd_packed(ctx.handle, byref(d), _ptr(codes), _ptr(scales), _ptr(residual), _ptr(dy), _ptr(gamma), _ptr(beta),
+                                      _ptr(save_mean), _ptr(save_rstd), _ptr(dx), _ptr(dresidual), _ptr(dgamma), _ptr(dbeta), _ptr(y), p, n,
+                                      _stream(stream)), "pt_gn_act_bwd_packed")
+
+
+def make_pack_desc(npix, C, ld=None, ldq=None) -> pt_pack_desc:
+    p8 = (C + 7) // 8 * 8
+    return pt_pack_desc(npix, C, ld or p8, ldq or p8)
+
+
+def pt_act_scale_bytes(npix: int, C: int) -> int:
+    return int(lib().pt_act_scale_bytes(npix, C))
+
+
+def checkpoint_buffers(npix: int, C: int, ldq=None, device="cuda"):
+    """Tensors for a checkpoint of npix pixels of C channels: codes int8 [npix][ldq], and the scale bytes."""
+    import torch
+    return (torch.empty((npix, ldq or (C + 7) // 8 * 8), dtype=torch.int8, device=device),
+            torch.empty(pt_act_scale_bytes(npix, C), dtype=torch.uint8, device=device))
+
+
+def pt_act_pack(ctx, d, x, codes, scales, stream=None):
+    _check(lib().pt_act_pack(ctx.handle, byref(d), _ptr(x), _ptr(codes), _ptr(scales), _stream(stream)), "pt_act_pack")
+
+
+def pt_act_unpack(ctx, d, codes, scales, x, stream=None):
+    _check(lib().pt_act_unpack(ctx.handle, byref(d), _ptr(codes), _ptr(scales), _ptr(x), _stream(stream)), "pt_act_unpack")
 
 
 def make_pool_desc(N, H, W, C, ld=None, R=3, stride=2, pad=1) -> pt_pool_desc:

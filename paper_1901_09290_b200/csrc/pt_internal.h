@@ -141,6 +141,11 @@ struct pt_ctx {
 
 static inline int pt_ceil_div(int a, int b) { return (a + b - 1) / b; }
 static inline size_t pt_align_up(size_t a, size_t b) { return (a + b - 1) / b * b; }
+// Whether the calling thread's current device is the context's (a launch goes to the current device, whatever the stream's).
+static inline bool pt_on_device(const pt_ctx *c) {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess && dev == c->device;
+}
 static inline int pt_out_dim(int H, int R, int stride, int pad) {
     int t = H + 2 * pad - R;
     return t < 0 ? 0 : t / stride + 1;
