@@ -2,20 +2,47 @@
 // activations with channel pitch ld, fp32 statistics and parameters. Per image n and group g of m = H*W*|g| values:
 //   forward : mean, rstd = 1/sqrt(var + eps), z = gamma*(x - mean)*rstd + beta (+ residual), y = act(z)
 //   backward: dz = dy*act'(z), A = sum gamma*dz, B = sum gamma*dz*xhat, dx = rstd*(gamma*dz - A/m - xhat*B/m)
-// A thread block per image reads its pixels twice, once for the sums and once for the results. No atomics: sums in a fixed order.
+// Both directions need an image's sums before its first result, and are bound by HBM: the aim is to read an image once.
+//
+// A thread-block cluster owns an image; each of its blocks owns a run of consecutive pixels, and a thread of a block a 16-byte vector
+// column and every so many-th pixel. Threads bring in what they will use themselves, by asynchronous copies into places of their own in
+// shared memory, a ring of batches of two pixels: there is nobody to wait for but one's own copies. A thread walks its pixels forwards for
+// the sums; the blocks of the cluster exchange the groups' sums through distributed shared memory; and it walks the pixels BACKWARDS for
+// the results: the last batches of the first walk are still in the ring, all of them where the image fits the cluster, and the others
+// were read recently enough to be in L2. Batches that the second walk is done with make room for the next image of the cluster.
+// No atomics: sums in a fixed order (run-to-run identical).
+//   (The first form had a producer warp and bulk copies of whole chunks of pixels. One thread issues such a copy every 0.3 to 0.5 us, which
+// with two or three tensors was the bound: 150 to 260 us for the backward pass at 64x28x28x371 with a residual, by the chunk's size.)
 #include "pt_internal.h"
 #include "pt_act.cuh"
+#include "pt_sm100_ptx.cuh"
 
 namespace {
 
-constexpr int kGnThreads = 256;
+constexpr int kGnThreads = 256;              // most consumer threads of a block (a producer warp follows them)
 constexpr int kGnTable = 256;                // most groups of a table
 constexpr int kGnMaxLd = 2048;
+constexpr int kGnMaxCluster = 16;
+constexpr int kGnExchange = 512;             // most entries (blocks of the cluster x groups) of one exchange buffer
+constexpr int kGnRows = 2;                   // pixels of a thread's batch
+
+enum { kGnFwd = 0, kGnFwdPack = 1, kGnBwd = 2, kGnBwdPacked = 3 };
+
+__host__ __device__ constexpr bool gn_bwd(int mode) { return mode >= kGnBwd; }
+// Bytes of a thread's place for one pixel: the vectors of x (or codes and the word that holds the scale byte), dy and the residual.
+__host__ __device__ constexpr int gn_slot(int mode, bool res) { return (mode == kGnBwdPacked ? 12 : 16) + (gn_bwd(mode) ? 16 : 0) + (gn_bwd(mode) && res ? 16 : 0); }
+// Batches of a thread's ring: what two blocks to an SM have room for.
+__host__ __device__ constexpr int gn_batches(int mode, bool res) { return 280 / (kGnRows * gn_slot(mode, res)); }
+constexpr int kGnBlocks = 2;                 // blocks of an SM: while one exchanges its sums, the other one moves data
 
 struct GnP {
     int N, HW, C, ld, LV, ldq, nb, G;
-    int w, rl, ppb;              // lanes of a checkpoint's block, lanes of a pixel, pixels the threads cover at a time
-    int act, table;
+    int w, rl, ppb, threads;     // lanes of a checkpoint's block, lanes of a pixel, pixels the threads cover at a time, threads
+    int pieces;                  // parts of the threads' sums of a channel that are added side by side
+    int gl;                      // lanes that add up a group
+    int cl, clusters, share;     // blocks of a cluster, clusters, pixels of a block
+    int table;
+    unsigned sm_gid, sm_gam, sm_bet, sm_grp, sm_chan, sm_red, sm_xch, sm_acc, sm_ring;
     float eps;
     uint16_t begin[kGnTable + 1];
 };
@@ -27,192 +54,658 @@ struct GnArgs {
     float *save_mean, *save_rstd;
     uint4 *y, *dx, *dres;
     uint8_t *codes, *scales;
-    float *rows;                 // backward: [N][2][ld] sums of dz and dz * xhat
+    double *rows;                // backward: [clusters][2][ld] sums of dz and dz * xhat over a cluster's images
+    float *dgamma, *dbeta;
 };
 
 __device__ __forceinline__ int group_begin(const GnP &p, int g) { return p.table ? p.begin[g] : g * (p.C / p.G); }
 
-__device__ __forceinline__ float sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
-
-__device__ __forceinline__ float activate(float z, int act)
+// ---- pairs of fp32 values in one 64-bit register: one instruction adds or multiplies both
+struct f2 { unsigned long long v; };
+__device__ __forceinline__ f2 mk2(float a, float b) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void un2(f2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x.v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return r; }
+// two bf16 as fp32
+__device__ __forceinline__ f2 from_bf(uint32_t w) { return mk2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ uint32_t to_bf(f2 x)
 {
-    if (act == PT_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-    return act == PT_ACT_SILU ? z * sigmoid(z) : z;
+    float a, b;
+    un2(x, a, b);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// z > 0, decided in 64 bits where fp32 might be wrong about it.
-__device__ __forceinline__ bool positive(float x, float mean, float rstd, float gamma, float beta, float r)
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+// sigmoid of a pair, 1/(1 + exp(-z)): one reciprocal serves both, 1/a = b/(a*b), which is one of the three operations per value that go
+// through the special-function units (16 lanes a cycle: at the rate HBM brings values they are two thirds busy in the backward pass). Below
+// -40 the sigmoid is taken at -40 (4e-18), which keeps a*b finite. Off by 2 ulp and |z| * 2^-24. (A NaN does not come through: the result
+// is only ever multiplied by z.)
+__device__ __forceinline__ f2 sigmoid2(f2 z)
 {
-    const float u = (x - mean) * (gamma * rstd), z = u + beta + r;
-    if (fabsf(z) > 1e-5f * (fabsf(u) + fabsf(r))) return z > 0.f;
-    return ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)beta + (double)r > 0.0;
+    float a, b;
+    un2(mul2(z, mk2(-1.4426950408889634f, -1.4426950408889634f)), a, b);           // -z * log2(e)
+    const f2 e = add2(mk2(ex2(fminf(a, 57.7f)), ex2(fminf(b, 57.7f))), mk2(1.f, 1.f));
+    un2(e, a, b);
+    const float r = rcp(a * b);
+    return mk2(r * b, r * a);
 }
 
-template <bool BWD>
-__global__ void __launch_bounds__(kGnThreads) gn_kernel(const __grid_constant__ GnP p, const GnArgs a)
+template <int ACT>
+__device__ __forceinline__ f2 activate2(f2 z)
 {
-    extern __shared__ float sm[];
-    float *red = sm;                                     // [threads][16]
-    double *chan = reinterpret_cast<double *>(sm + kGnThreads * 16);     // [2][ld]
-    float *g0 = reinterpret_cast<float *>(chan + 2 * p.ld), *g1 = g0 + p.ld, *g2 = g1 + p.ld, *g3 = g2 + p.ld;       // per channel, from its group
-    const int t = threadIdx.x, pr = t / p.rl, cv = t - pr * p.rl, n = blockIdx.x;
-    const bool lane_ok = pr < p.ppb && cv < p.LV;
-    const size_t base = (size_t)n * p.HW;
-    const int c0 = cv * 8;
+    if (ACT == PT_ACT_NONE) return z;
+    if (ACT == PT_ACT_SILU) return mul2(z, sigmoid2(z));
+    float a, b;
+    un2(z, a, b);
+    return mk2(a > 0.f ? a : (a != a ? a : 0.f), b > 0.f ? b : (b != b ? b : 0.f));
+}
+
+// Two fp64 values into the shared memory of another block of the cluster, visible there behind the cluster's barrier.
+__device__ __forceinline__ void st_cluster_2d(uint32_t addr, double a, double b)
+{
+    asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(addr), "d"(a), "d"(b) : "memory");
+}
+__device__ __forceinline__ double ld_cluster_d(uint32_t addr)
+{
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+    return v;
+}
+// Asynchronous copies of a thread, in groups; waiting for all but the last `PENDING` groups.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy8(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
+// The largest bf16 <= v (its bits): x > v exactly where x > that, for every bf16 x.
+__device__ __forceinline__ uint32_t bf16_floor(double v)
+{
+    const uint32_t u = __float_as_uint(__double2float_rd(v));
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;                 // NaN: no x is above it
+    return (u >> 31) ? ((u + 0xffffu) >> 16) : (u >> 16);                // (towards -inf: a negative one's magnitude rounds up)
+}
+
+// Which of two neighbouring values (bf16 halves of x) have z = gamma*xhat + beta + residual > 0, in 64 bits. Rarely called: fp32 decides
+// everywhere but next to 0.
+__device__ __noinline__ uint32_t exact_mask(uint32_t x, uint32_t r, int c, const uint16_t *gid, const float *grp, int G, const float *gam, const float *bet)
+{
+    uint32_t m = 0u;
+    for (int h = 0; h < 2; ++h) {
+        const int g = gid[c + h];
+        const double xv = (double)__uint_as_float(h ? x & 0xffff0000u : x << 16), rv = (double)__uint_as_float(h ? r & 0xffff0000u : r << 16);
+        if ((xv - (double)grp[g]) * (double)grp[G + g] * (double)gam[c + h] + (double)bet[c + h] + rv > 0.0) m |= h ? 0xffff0000u : 0xffffu;
+    }
+    return m;
+}
+
+// Eight restored values as pairs (act8::decode8), and two of them as bf16, in which they are exact: their upper halves.
+__device__ __forceinline__ void decode8(const uint2 &q, uint32_t byte, f2 (&x)[4])
+{
+    const float s = act8::scale_of(byte);
+    const f2 bias = mk2(-8388736.f, -8388736.f), ss = mk2(s, s);
+    const uint32_t a = q.x ^ 0x80808080u, b = q.y ^ 0x80808080u;
+    x[0] = mk2(__uint_as_float(__byte_perm(a, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(a, 0x4b000000u, 0x7441)));
+    x[1] = mk2(__uint_as_float(__byte_perm(a, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(a, 0x4b000000u, 0x7443)));
+    x[2] = mk2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7441)));
+    x[3] = mk2(__uint_as_float(__byte_perm(b, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(b, 0x4b000000u, 0x7443)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = mul2(add2(x[i], bias), ss);
+}
+__device__ __forceinline__ uint32_t exact_bf(f2 x)
+{
+    float a, b;
+    un2(x, a, b);
+    return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632);
+}
+
+// What a thread reads of one pixel: its vector of x (or of codes, with the block's scale byte), of dy and of the residual.
+struct Raw {
+    uint4 x, dy, res;
+    uint2 q;
+    uint32_t byte;
+};
+
+template <int MODE, int ACT, bool RES>
+__global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_constant__ GnP p, const GnArgs a)
+{
+    constexpr bool BWD = gn_bwd(MODE), PACK = MODE == kGnFwdPack, PACKED = MODE == kGnBwdPacked;
+    constexpr int B = gn_batches(MODE, RES), U = kGnRows;
+    // the ring's parts, [B][U][threads] each: x or codes, dy, residual, scale words
+    constexpr uint32_t kXs = PACKED ? 8 : 16, kRowX = kGnThreads * kXs, kRow = kGnThreads * 16, kRowS = kGnThreads * 4;
+    constexpr uint32_t kDy = B * U * kRowX, kRes = kDy + (BWD ? B * U * kRow : 0), kSc = kRes + (BWD && RES ? B * U * kRow : 0);
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint16_t *gid = reinterpret_cast<uint16_t *>(smem + p.sm_gid);       // [ld] group of a channel
+    float *gam = reinterpret_cast<float *>(smem + p.sm_gam), *bet = reinterpret_cast<float *>(smem + p.sm_bet);      // [ld]
+    float *grps = reinterpret_cast<float *>(smem + p.sm_grp);            // [2][2][G] of alternating images: mean and rstd (backward), pivot
+    float *out = grps + 4 * p.G;                                         // [2][G] rstd and mean (forward), the group's terms of dx (backward)
+    float *chan = reinterpret_cast<float *>(smem + p.sm_chan);           // [pieces][2][8 LV]
+    float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][17]
+    double2 *xch = reinterpret_cast<double2 *>(smem + p.sm_xch);         // [2][cl][G]
+    double *acc = reinterpret_cast<double *>(smem + p.sm_acc);           // [2][ld]
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = p.threads >> 5;
+    const int rank = (int)(blockIdx.x % p.cl), cluster = (int)(blockIdx.x / p.cl);
+    const int first = rank * p.share, mine = p.HW - first < p.share ? (p.HW - first > 0 ? p.HW - first : 0) : p.share;
+    const int step = U * p.ppb, NB = (mine + step - 1) / step;           // pixels and number of the block's batches
+    const int pr = t / p.rl, cv = t - pr * p.rl, c0 = cv * 8;
+    const bool lane_ok = pr < p.ppb && cv < p.LV, has = lane_ok && c0 < p.C;     // has: the vector holds channels, not pad lanes only
     const uint4 keep = act8::keep_bits(c0, p.C);
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    if (BWD) {
-        for (int g = t; g < p.G; g += kGnThreads)
-            for (int c = group_begin(p, g); c < group_begin(p, g + 1); ++c) {
-                g0[c] = a.mean[(size_t)n * p.G + g];
-                g1[c] = a.rstd[(size_t)n * p.G + g];
-            }
-    } else {
-        for (int g = t; g < p.G; g += kGnThreads) {      // pivot: the group's first value in the image
-            const float v = __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(a.x)[base * p.ld + group_begin(p, g)]);
-            for (int c = group_begin(p, g); c < group_begin(p, g + 1); ++c) g0[c] = v;
-        }
-    }
-    __syncthreads();
-    float s0[8], s1[8], k0[8], k1[8], gam[8], bet[8];
+    const uint8_t *mine_x = smem + p.sm_ring + t * kXs, *mine_v = smem + p.sm_ring + t * 16, *mine_s = smem + p.sm_ring + kSc + t * 4;
+    const uint32_t to_x = sm100::smem_u32(mine_x), to_v = sm100::smem_u32(mine_v), to_s = sm100::smem_u32(mine_s);
+    for (int g = t; g < p.G; g += p.threads)
+        for (int c = group_begin(p, g), e = group_begin(p, g + 1); c < e; ++c) gid[c] = (uint16_t)g;
+    for (int c = p.C + t; c < p.ld; c += p.threads) gid[c] = (uint16_t)(p.G - 1);
+    sm100::grid_dependency_wait();
+    sm100::grid_launch_dependents();
+    // batch b of image n into the ring's place s
+    const auto bring = [&](int n, int b, int s) {
+        if (has && n < p.N && b < NB) {
+            const int r0 = b * step + pr;
+            const size_t pix0 = (size_t)n * p.HW + first;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const bool ok = lane_ok && c0 + j < p.C;
-        s0[j] = s1[j] = 0.f;
-        k0[j] = ok ? g0[c0 + j] : 0.f;
-        k1[j] = ok && BWD ? g1[c0 + j] : 0.f;
-        gam[j] = ok ? a.gamma[c0 + j] : 0.f;
-        bet[j] = ok ? a.beta[c0 + j] : 0.f;
-    }
-    const auto load_x = [&](size_t pix, float (&f)[8]) {
-        if (BWD && a.codes_in) act8::decode8(*reinterpret_cast<const uint2 *>(a.codes_in + pix * p.ldq + c0), a.scales_in[pix * p.nb + (cv >> 2)], f);
-        else act8::unpack8(a.x[pix * (p.ld / 8) + cv], f);
-    };
-    const auto load_dz = [&](size_t pix, const float (&x)[8], float (&dz)[8], float (&z)[8]) {
-        float r[8];
-        act8::unpack8(a.dy[pix * (p.ld / 8) + cv], dz);
-        if (a.res) act8::unpack8(a.res[pix * (p.ld / 8) + cv], r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float rj = a.res ? r[j] : 0.f;
-            z[j] = fmaf(x[j] - k0[j], gam[j] * k1[j], bet[j]) + rj;
-            if (p.act == PT_ACT_RELU) dz[j] = positive(x[j], k0[j], k1[j], gam[j], bet[j], rj) ? dz[j] : 0.f;
-            if (p.act == PT_ACT_SILU) { const float s = sigmoid(z[j]); dz[j] *= fmaf(z[j] * s, 1.f - s, s); }
-        }
-    };
-    for (int q0 = 0; q0 < p.HW; q0 += p.ppb) {
-        const int q = q0 + pr;
-        const bool ok = lane_ok && q < p.HW;
-        const size_t pix = base + q;
-        float x[8];
-        if (BWD) {
-            if (!ok || c0 >= p.C) continue;
-            float dz[8], z[8];
-            load_x(pix, x);
-            load_dz(pix, x, dz, z);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { s0[j] += dz[j]; s1[j] = fmaf(dz[j], x[j] - k0[j], s1[j]); }
-        } else {
-            const uint4 v = ok ? a.x[pix * (p.ld / 8) + cv] : zero;
-            act8::unpack8(v, x);
-            if (ok)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { const float d = x[j] - k0[j]; s0[j] += d; s1[j] = fmaf(d, d, s1[j]); }
-            if (a.codes) {
-                const uint4 m = act8::and4(v, keep);
-                const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(m), p.w));
-                if (ok && c0 < p.C) {
-                    *reinterpret_cast<uint2 *>(a.codes + pix * p.ldq + c0) = act8::encode8(m, byte);
-                    if ((cv & 3) == 0) a.scales[pix * p.nb + (cv >> 2)] = (uint8_t)byte;
+            for (int u = 0; u < U; ++u) {
+                const int r = r0 + u * p.ppb;
+                if (r < mine) {
+                    const size_t pix = pix0 + r, at = pix * p.LV + cv;
+                    if (PACKED) {
+                        const size_t sc = pix * p.nb + (cv >> 2);
+                        copy8(to_x + (uint32_t)(s * U + u) * kRowX, a.codes_in + pix * p.ldq + c0);
+                        copy4(to_s + (uint32_t)(s * U + u) * kRowS, a.scales_in + (sc & ~(size_t)3));
+                    } else {
+                        copy16(to_x + (uint32_t)(s * U + u) * kRowX, a.x + at);
+                    }
+                    if (BWD) copy16(to_v + kDy + (uint32_t)(s * U + u) * kRow, a.dy + at);
+                    if (BWD && RES) copy16(to_v + kRes + (uint32_t)(s * U + u) * kRow, a.res + at);
                 }
             }
         }
+        copy_commit();
+    };
+#pragma unroll 1
+    for (int b = 0; b < B; ++b) bring(cluster, b, b);
+    for (int c = t; c < p.ld; c += p.threads) {
+        gam[c] = c < p.C ? a.gamma[c] : 0.f;
+        bet[c] = c < p.C ? a.beta[c] : 0.f;
+        if (BWD) acc[c] = acc[p.ld + c] = 0.0;
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { red[t * 16 + j] = s0[j]; red[t * 16 + 8 + j] = s1[j]; }
-    __syncthreads();
-    for (int e = t; e < 2 * p.C; e += kGnThreads) {
-        const int s = e >= p.C, c = e - s * p.C;
-        double v = 0.0;
-        for (int r = 0; r < p.ppb; ++r) v += (double)red[(r * p.rl + (c >> 3)) * 16 + s * 8 + (c & 7)];
-        if (BWD && s) v *= (double)g1[c];
-        chan[s * p.ld + c] = v;
-        if (BWD) a.rows[((size_t)n * 2 + s) * p.ld + c] = (float)v;
-    }
-    __syncthreads();
-    for (int g = t; g < p.G; g += kGnThreads) {
-        const int b = group_begin(p, g), e = group_begin(p, g + 1);
-        const double m = (double)p.HW * (double)(e - b);
-        double v0 = 0.0, v1 = 0.0;
-        for (int c = b; c < e; ++c) {
-            const double f = BWD ? (double)a.gamma[c] : 1.0;
-            v0 += f * chan[c];
-            v1 += f * chan[p.ld + c];
-        }
-        float f0, f1;
-        if (BWD) {
-            const double r = (double)g1[b];
-            f0 = (float)(r * v0 / m);
-            f1 = (float)(r * r * v1 / m);
+    int dir = 0, it = 0;
+    const double inv_hw = 1.0 / (double)p.HW;
+    const bool ahead = BWD && p.G <= p.threads;                          // the next image's statistics are fetched during the second walk
+    float next_mean = 0.f, next_rstd = 0.f;
+    for (int n = cluster; n < p.N; n += p.clusters, dir ^= 1, ++it) {
+        const size_t base = (size_t)n * p.HW + first;                    // the block's first pixel
+        // (so that a batch of the first walk always has B - 1 groups behind it when it is waited for)
+        if (it > 0)
+            for (int b = NB; b < B; ++b) copy_commit();
+        // ---- what the first walk needs of every group: the statistics (backward), or a value near its mean (forward)
+        float *grp = grps + (it & 1) * 2 * p.G;
+        if (BWD && ahead && it > 0) {
+            if (t < p.G) { grp[t] = next_mean; grp[p.G + t] = next_rstd; }
+        } else if (BWD) {
+            for (int g = t; g < p.G; g += p.threads) {
+                grp[g] = a.mean[(size_t)n * p.G + g];
+                grp[p.G + g] = a.rstd[(size_t)n * p.G + g];
+            }
         } else {
-            const double d = v0 / m;
-            double var = v1 / m - d * d;
-            if (var < 0.0) var = 0.0;
-            f0 = (float)((double)g0[b] + d);
-            f1 = (float)(1.0 / sqrt(var + (double)p.eps));
-            a.save_mean[(size_t)n * p.G + g] = f0;
-            a.save_rstd[(size_t)n * p.G + g] = f1;
-        }
-        for (int c = b; c < e; ++c) { g2[c] = f0; g3[c] = f1; }
-    }
-    __syncthreads();
-    float k2[8], k3[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const bool ok = lane_ok && c0 + j < p.C;
-        k2[j] = ok ? g2[c0 + j] : 0.f;
-        k3[j] = ok ? g3[c0 + j] : 0.f;
-    }
-    if (!lane_ok) return;
-    for (int q = pr; q < p.HW; q += p.ppb) {
-        const size_t pix = base + q, at = pix * (p.ld / 8) + cv;
-        float x[8], o[8];
-        if (c0 >= p.C) {                                 // vectors of pad lanes only
-            if (BWD) { a.dx[at] = zero; if (a.dres) a.dres[at] = zero; }
-            if (a.y) a.y[at] = zero;
-            continue;
-        }
-        load_x(pix, x);
-        if (!BWD) {
-            float r[8];
-            if (a.res) act8::unpack8(a.res[at], r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = activate(fmaf(x[j] - k2[j], gam[j] * k3[j], bet[j]) + (a.res ? r[j] : 0.f), p.act);
-            a.y[at] = act8::and4(act8::pack8(o), keep);
-        } else {
-            float dz[8], z[8];
-            load_dz(pix, x, dz, z);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = fmaf(gam[j] * k1[j], dz[j], -fmaf(x[j] - k0[j], k3[j], k2[j]));
-            a.dx[at] = act8::and4(act8::pack8(o), keep);
-            if (a.dres) a.dres[at] = act8::and4(act8::pack8(dz), keep);
-            if (a.y) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = activate(z[j], p.act);
-                a.y[at] = act8::and4(act8::pack8(o), keep);
+            copy_wait<B - 1>();
+            __syncthreads();
+            // the average over the group's channels of the block's first pixels: as near the mean as a few values tell
+            const int rows = min(min(4, p.ppb), mine), per = 32 / p.gl, l = lane & (p.gl - 1);
+            const uint8_t *px = smem + p.sm_ring + (dir ? (B - 1) * U * kRowX : 0u);
+            for (int g0 = warp * per; g0 < p.G; g0 += warps * per) {
+                const int g = g0 + lane / p.gl;
+                const int b = g < p.G ? group_begin(p, g) : 0, e = g < p.G ? group_begin(p, g + 1) : 0;
+                float v = 0.f;
+                for (int c = b + l; c < e; c += p.gl)
+                    for (int r = 0; r < rows; ++r)
+                        v += __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(px + (size_t)(r * p.rl + (c >> 3)) * 16 + (c & 7) * 2));
+                for (int o = p.gl >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                if (l == 0 && g < p.G) grp[g] = rows > 0 ? v / (float)(rows * (e - b)) : 0.f;
             }
         }
+        __syncthreads();
+        // the thread's constants: minus the mean (or pivot), and in the backward pass gamma*rstd, beta, and the ReLU's limits as bf16: without
+        // a residual, z > 0 exactly where x ^ sgn > thr
+        f2 nm[4], k[4], be[4];
+        uint32_t thr[4], sgn[4];
+        float be_max = 0.f;
+        {
+            float m[8], kk[8], b[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = has ? c0 + j : 0, g = gid[c];
+                m[j] = -grp[g];
+                if (BWD) {
+                    kk[j] = gam[c] * grp[p.G + g];
+                    b[j] = bet[c];
+                    be_max = fmaxf(be_max, fabsf(b[j]));
+                }
+                if (BWD && ACT == PT_ACT_RELU && !RES) {
+                    // z = s*(x - mean) + beta > 0  <=>  x > mean - beta/s (s > 0), -x > -(mean - beta/s) (s < 0); a constant for s = 0
+                    const double s = (double)gam[c] * (double)grp[p.G + g], bj = (double)bet[c];
+                    const double lim = s == 0.0 ? (bj > 0.0 ? -INFINITY : INFINITY) : (double)grp[g] - bj / s;
+                    const uint32_t th = bf16_floor(s < 0.0 ? -lim : lim), sg = s < 0.0 ? 0x8000u : 0u;
+                    thr[j >> 1] = j & 1 ? thr[j >> 1] | th << 16 : th;
+                    sgn[j >> 1] = j & 1 ? sgn[j >> 1] | sg << 16 : sg;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                nm[i] = mk2(m[2 * i], m[2 * i + 1]);
+                if (BWD) { k[i] = mk2(kk[2 * i], kk[2 * i + 1]); be[i] = mk2(b[2 * i], b[2 * i + 1]); }
+            }
+        }
+        // pixel u of the batch at the ring's place s; r: its number among the block's pixels
+        const auto fetch = [&](Raw &w, int s, int u, int r) {
+            if (PACKED) {
+                w.q = *reinterpret_cast<const uint2 *>(mine_x + (uint32_t)(s * U + u) * kRowX);
+                const uint32_t sc = (uint32_t)((base + r) * p.nb) + (uint32_t)(cv >> 2);
+                w.byte = *reinterpret_cast<const uint32_t *>(mine_s + (uint32_t)(s * U + u) * kRowS) >> ((sc & 3u) * 8u) & 0xffu;
+            } else {
+                w.x = *reinterpret_cast<const uint4 *>(mine_x + (uint32_t)(s * U + u) * kRowX);
+            }
+            if (BWD) w.dy = *reinterpret_cast<const uint4 *>(mine_v + kDy + (uint32_t)(s * U + u) * kRow);
+            if (BWD && RES) w.res = *reinterpret_cast<const uint4 *>(mine_v + kRes + (uint32_t)(s * U + u) * kRow);
+        };
+        const auto values = [&](Raw &w, f2 (&x)[4]) {                   // x as fp32 pairs (and, from codes, as bf16 words)
+            if (PACKED) {
+                decode8(w.q, w.byte, x);
+                if (ACT == PT_ACT_RELU) w.x = make_uint4(exact_bf(x[0]), exact_bf(x[1]), exact_bf(x[2]), exact_bf(x[3]));
+            } else {
+                x[0] = from_bf(w.x.x); x[1] = from_bf(w.x.y); x[2] = from_bf(w.x.z); x[3] = from_bf(w.x.w);
+            }
+        };
+        // dz: in place of dy's words where it is dy's bits under a mask, and as pairs. d = x - mean.
+        const auto gradient = [&](Raw &w, const f2 (&d)[4], f2 (&z)[4], f2 (&dz)[4], bool want_z) {
+            uint32_t *g = reinterpret_cast<uint32_t *>(&w.dy);
+            const uint32_t *xb = reinterpret_cast<const uint32_t *>(&w.x), *rb = reinterpret_cast<const uint32_t *>(&w.res);
+            if (ACT == PT_ACT_SILU || want_z || (ACT == PT_ACT_RELU && RES))
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[i] = fma2(d[i], k[i], be[i]);
+                    if (RES) z[i] = add2(z[i], from_bf(rb[i]));
+                }
+            if (ACT == PT_ACT_RELU && !RES) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t u = xb[i] ^ sgn[i];
+                    g[i] &= __hgt2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&thr[i]));
+                }
+            }
+            if (ACT == PT_ACT_RELU && RES) {
+                // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |beta| + |residual|: there 64 bits decide. One test for the
+                // eight values, the least |z| against the largest |residual|: it is passed a few times in a hundred thousand.
+                float zz[8], low = INFINITY;
+                uint32_t top = 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    un2(z[i], zz[2 * i], zz[2 * i + 1]);
+                    low = fminf(low, fminf(fabsf(zz[2 * i]), fabsf(zz[2 * i + 1])));
+                    top = __vmaxu2(top, rb[i] & 0x7fff7fffu);
+                }
+                const float rmax = fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u));
+                if (low <= 1e-6f * (rmax + be_max)) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // (gamma = 0, a pruned channel's or a pad lane's: z = beta + residual, of the right sign in fp32)
+                        float k0, k1, b0, b1;
+                        un2(k[i], k0, k1);
+                        un2(be[i], b0, b1);
+                        const bool near0 = k0 != 0.f && fabsf(zz[2 * i]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] << 16)) + fabsf(b0));
+                        const bool near1 = k1 != 0.f && fabsf(zz[2 * i + 1]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] & 0xffff0000u)) + fabsf(b1));
+                        uint32_t m = (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
+                        if (near0 || near1) m = exact_mask(xb[i], rb[i], (has ? c0 : 0) + 2 * i, gid, grp, p.G, gam, bet);
+                        g[i] &= m;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) g[i] &= (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                dz[i] = from_bf(g[i]);
+                if (ACT == PT_ACT_SILU) {                                // act' = s + z*s*(1 - s)
+                    const f2 s = sigmoid2(z[i]);
+                    dz[i] = mul2(dz[i], fma2(mul2(z[i], s), fma2(s, mk2(-1.f, -1.f), mk2(1.f, 1.f)), s));
+                }
+            }
+        };
+
+        // ---- first walk: sums of x - pivot and its square, or of dz and dz * (x - mean)
+        f2 s0[4], s1[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s0[i] = s1[i] = mk2(0.f, 0.f);
+        const auto count = [&](Raw &w) {
+            f2 x[4], z[4], dz[4];
+            values(w, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = add2(x[i], nm[i]);
+            if (BWD) gradient(w, x, z, dz, false);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f2 d = BWD ? dz[i] : x[i];
+                s0[i] = add2(s0[i], d);
+                s1[i] = fma2(d, x[i], s1[i]);
+            }
+        };
+        // a thread's chains of additions stay short: every 64 rows they go to its place in shared memory
+        bool flushed = false;
+        const auto flush = [&]() {
+            float *o = red + t * 17;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float u[4];
+                un2(s0[i], u[0], u[1]);
+                un2(s1[i], u[2], u[3]);
+                o[2 * i] = flushed ? o[2 * i] + u[0] : u[0];
+                o[2 * i + 1] = flushed ? o[2 * i + 1] + u[1] : u[1];
+                o[8 + 2 * i] = flushed ? o[8 + 2 * i] + u[2] : u[2];
+                o[9 + 2 * i] = flushed ? o[9 + 2 * i] + u[3] : u[3];
+                s0[i] = s1[i] = mk2(0.f, 0.f);
+            }
+            flushed = true;
+        };
+        int s = dir ? B - 1 : 0;
+        for (int b = 0; b < NB; ++b) {
+            copy_wait<B - 1>();
+            const int r0 = b * step + pr;
+            if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int r = r0 + u * p.ppb;
+                    const bool ok = has && r < mine;
+                    Raw w;
+                    w.x = make_uint4(0u, 0u, 0u, 0u);
+                    if (ok) {
+                        fetch(w, s, u, r);
+                        count(w);
+                    }
+                    w.x = act8::and4(w.x, keep);
+                    const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(w.x), p.w));
+                    if (ok) {
+                        *reinterpret_cast<uint2 *>(a.codes + (base + r) * p.ldq + c0) = act8::encode8(w.x, byte);
+                        if ((cv & 3) == 0) a.scales[(base + r) * p.nb + (cv >> 2)] = (uint8_t)byte;
+                    }
+                }
+            } else if (has) {
+                if ((b + 1) * step <= mine) {                            // two pixels at a time, their loads first
+                    Raw w[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) fetch(w[u], s, u, r0 + u * p.ppb);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) count(w[u]);
+                } else {
+#pragma unroll 1
+                    for (int u = 0; u < U; ++u)
+                        if (r0 + u * p.ppb < mine) {
+                            Raw w;
+                            fetch(w, s, u, r0 + u * p.ppb);
+                            count(w);
+                        }
+                }
+            }
+            if (b + B < NB) bring(n, b + B, s);                          // (the last B batches stay for the second walk)
+            else copy_commit();
+            if ((b & 31) == 31 || b == NB - 1) flush();
+            if (dir) s = s == 0 ? B - 1 : s - 1;
+            else s = s == B - 1 ? 0 : s + 1;
+        }
+        if (NB == 0) flush();
+        // ---- a channel's sums over the threads' rows, then a group's over its channels
+        __syncthreads();
+        const int cols = p.LV * 8;
+        for (int e = t; e < 2 * cols * p.pieces; e += p.threads) {
+            const int piece = e / (2 * cols), v = e - piece * 2 * cols, s = v >= cols ? 1 : 0, c = v - s * cols;
+            const float *src = red + (c >> 3) * 17 + s * 8 + (c & 7);
+            float u0 = 0.f, u1 = 0.f;
+            int r = piece;
+            for (; r + p.pieces < p.ppb; r += 2 * p.pieces) { u0 += src[r * p.rl * 17]; u1 += src[(r + p.pieces) * p.rl * 17]; }
+            if (r < p.ppb) u0 += src[r * p.rl * 17];
+            chan[e] = u0 + u1;
+        }
+        __syncthreads();
+        if (BWD)
+            for (int c = t; c < p.C; c += p.threads) {                 // the images' sums of dz and dz * xhat
+                double v0 = 0.0, v1 = 0.0;
+                for (int k = 0; k < p.pieces; ++k) { v0 += (double)chan[k * 2 * cols + c]; v1 += (double)chan[k * 2 * cols + cols + c]; }
+                acc[c] += v0;
+                acc[p.ld + c] += v1 * (double)grp[p.G + gid[c]];
+            }
+        {
+            const int per = 32 / p.gl, l = lane & (p.gl - 1), buf = it & 1;
+            for (int g0 = warp * per; g0 < p.G; g0 += warps * per) {
+                const int g = g0 + lane / p.gl;
+                const int b = g < p.G ? group_begin(p, g) : 0, e = g < p.G ? group_begin(p, g + 1) : 0;
+                double v0 = 0.0, v1 = 0.0;
+                for (int c = b + l; c < e; c += p.gl) {
+                    double w0 = 0.0, w1 = 0.0;
+                    for (int k = 0; k < p.pieces; ++k) { w0 += (double)chan[k * 2 * cols + c]; w1 += (double)chan[k * 2 * cols + cols + c]; }
+                    const double f = BWD ? (double)gam[c] : 1.0;
+                    v0 += f * w0;
+                    v1 += f * w1;
+                }
+                for (int o = p.gl >> 1; o; o >>= 1) {
+                    v0 += __shfl_xor_sync(0xffffffffu, v0, o);
+                    v1 += __shfl_xor_sync(0xffffffffu, v1, o);
+                }
+                if (!BWD) {                                              // the block's mean and sum of squares about it
+                    const double cnt = (double)mine * (double)(e - b), d = cnt > 0.0 ? v0 / cnt : 0.0;
+                    v1 = v1 - v0 * d;
+                    v0 = g < p.G && mine > 0 ? (double)grp[g] + d : 0.0;
+                    if (v1 < 0.0) v1 = 0.0;
+                }
+                if (g < p.G)
+                    for (int r = l; r < p.cl; r += p.gl) {
+                        double2 *to = xch + ((size_t)buf * p.cl + rank) * p.G + g;
+                        if (p.cl == 1) *to = make_double2(v0, v1);
+                        else st_cluster_2d(sm100::map_to_rank(sm100::smem_u32(to), (uint32_t)r), v0, v1);
+                    }
+            }
+            if (p.cl > 1) sm100::cluster_barrier();
+            else __syncthreads();
+            // ---- the image's values from those of the cluster's blocks, in order
+            for (int g = t; g < p.G; g += p.threads) {
+                const double2 *v = xch + (size_t)buf * p.cl * p.G + g;
+                const int size = group_begin(p, g + 1) - group_begin(p, g);
+                const double m = (double)p.HW * (double)size;
+                double v0 = 0.0, v1 = 0.0;
+                if (BWD) {
+                    for (int r = 0; r < p.cl; ++r) { v0 += v[(size_t)r * p.G].x; v1 += v[(size_t)r * p.G].y; }
+                    const double rs = (double)grp[p.G + g], im = 1.0 / m;
+                    out[g] = -(float)(rs * v0 * im);
+                    out[p.G + g] = -(float)(rs * rs * rs * v1 * im);
+                } else {
+                    const auto cnt = [&](int r) { const int c = p.HW - r * p.share; return (double)(c < 0 ? 0 : c < p.share ? c : p.share); };
+                    for (int r = 0; r < p.cl; ++r) v0 += v[(size_t)r * p.G].x * (cnt(r) * inv_hw);
+                    for (int r = 0; r < p.cl; ++r) {
+                        const double d = v[(size_t)r * p.G].x - v0;
+                        v1 += v[(size_t)r * p.G].y + d * d * (cnt(r) * (double)size);
+                    }
+                    const float fm = (float)v0, fr = (float)rsqrt(v1 / m + (double)p.eps);
+                    out[g] = fr;
+                    out[p.G + g] = fm;
+                    if (rank == 0) {
+                        a.save_mean[(size_t)n * p.G + g] = fm;
+                        a.save_rstd[(size_t)n * p.G + g] = fr;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        // the second walk's constants: forward, minus the mean, gamma*rstd and beta; backward, the group's terms of dx
+        f2 c1[4], c2[4];
+        {
+            float u[8], v[8], m[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = has ? c0 + j : 0, g = gid[c];
+                u[j] = out[g];
+                v[j] = out[p.G + g];
+                if (!BWD) {
+                    m[j] = -v[j];
+                    u[j] *= gam[c];
+                    v[j] = bet[c];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c1[i] = mk2(u[2 * i], u[2 * i + 1]);
+                c2[i] = mk2(v[2 * i], v[2 * i + 1]);
+                if (!BWD) nm[i] = mk2(m[2 * i], m[2 * i + 1]);
+            }
+        }
+        if (ahead && t < p.G && n + p.clusters < p.N) {
+            next_mean = a.mean[(size_t)(n + p.clusters) * p.G + t];
+            next_rstd = a.rstd[(size_t)(n + p.clusters) * p.G + t];
+        }
+        // ---- second walk, backwards: the results
+        const bool want_y = !BWD || (PACKED && a.y);
+        const auto result = [&](Raw &w, const size_t at) {
+            f2 x[4], z[4], dz[4];
+            uint4 o;
+            uint32_t *ow = reinterpret_cast<uint32_t *>(&o);
+            values(w, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = add2(x[i], nm[i]);
+            if (!BWD) {
+                const uint32_t *rb = reinterpret_cast<const uint32_t *>(&w.res);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    f2 y = fma2(x[i], c1[i], c2[i]);
+                    if (RES) y = add2(y, from_bf(rb[i]));
+                    ow[i] = to_bf(activate2<ACT>(y));
+                }
+                a.y[at] = act8::and4(o, keep);
+            } else {
+                gradient(w, x, z, dz, want_y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ow[i] = to_bf(fma2(k[i], dz[i], fma2(x[i], c2[i], c1[i])));
+                a.dx[at] = act8::and4(o, keep);
+                if (a.dres) {
+                    if (ACT == PT_ACT_SILU) w.dy = make_uint4(to_bf(dz[0]), to_bf(dz[1]), to_bf(dz[2]), to_bf(dz[3]));
+                    a.dres[at] = act8::and4(w.dy, keep);
+                }
+                if (want_y) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ow[i] = to_bf(activate2<ACT>(z[i]));
+                    a.y[at] = act8::and4(o, keep);
+                }
+            }
+        };
+        Raw ahead_w[U];                                                  // forward: the residual, a batch ahead
+        const auto residual = [&](int b) {
+            if (!BWD && RES && has && b >= 0)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int r = b * step + u * p.ppb + pr;
+                    if (r < mine) ahead_w[u].res = a.res[(base + r) * p.LV + cv];
+                }
+        };
+        residual(NB - 1);
+        const int keep_b = NB < B ? NB : B;
+        for (int b = NB - 1; b >= 0; --b) {
+            if (dir) s = s == B - 1 ? 0 : s + 1;
+            else s = s == 0 ? B - 1 : s - 1;
+            copy_wait<B - 1>();
+            const int r0 = b * step + pr;
+            Raw w[U];
+            if (!BWD && RES) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) w[u].res = ahead_w[u].res;
+                residual(b - 1);
+            }
+            if (has) {
+                if ((b + 1) * step <= mine) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) fetch(w[u], s, u, r0 + u * p.ppb);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) result(w[u], (base + r0 + u * p.ppb) * p.LV + cv);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (r0 + u * p.ppb < mine) {
+                            fetch(w[u], s, u, r0 + u * p.ppb);
+                            result(w[u], (base + r0 + u * p.ppb) * p.LV + cv);
+                        }
+                }
+            } else if (lane_ok) {                                        // vectors of pad lanes only
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                for (int u = 0; u < U; ++u) {
+                    if (r0 + u * p.ppb >= mine) continue;
+                    const size_t at = (base + r0 + u * p.ppb) * p.LV + cv;
+                    if (BWD) { a.dx[at] = zero; if (a.dres) a.dres[at] = zero; }
+                    if (want_y) a.y[at] = zero;
+                }
+            }
+            if (b >= B) bring(n, b - B, s);
+            else bring(n + p.clusters, keep_b - 1 - b, dir ? keep_b - 1 - b : B - keep_b + b);
+        }
+    }
+    // ---- the cluster's sums over its images
+    if (BWD) {
+        if (p.cl > 1) sm100::cluster_barrier();
+        else __syncthreads();
+        const int per = (2 * p.ld + p.cl - 1) / p.cl;
+        for (int e = rank * per + t; e < min(2 * p.ld, (rank + 1) * per); e += p.threads) {
+            double v = 0.0;
+            if (p.cl == 1) v = acc[e];
+            else
+                for (int r = 0; r < p.cl; ++r) v += ld_cluster_d(sm100::map_to_rank(sm100::smem_u32(acc + e), (uint32_t)r));
+            const int s = e >= p.ld, c = e - s * p.ld;
+            if (p.clusters > 1) a.rows[(size_t)cluster * 2 * p.ld + e] = v;
+            else if (c < p.C) (s ? a.dgamma : a.dbeta)[c] = (float)v;
+        }
+    }
+    if (p.cl > 1) sm100::cluster_barrier();
+}
+
+// dgamma, dbeta: the clusters' rows. A block owns 32 columns; its warps take every 32nd row each, then one thread per column adds the
+// warps' sums: a fixed order, fp64.
+__global__ void __launch_bounds__(1024) gn_finish_kernel(const double *rows, int n, int C, int ld, float *dgamma, float *dbeta)
+{
+    __shared__ double part[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
+    sm100::grid_dependency_wait();
+    sm100::grid_launch_dependents();
+    double v = 0.0;
+    if (e < 2 * ld)
+        for (int r = warp; r < n; r += 32) v += rows[(size_t)r * 2 * ld + e];
+    part[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && e < 2 * ld) {
+        v = 0.0;
+        for (int k = 0; k < 32; ++k) v += part[k][lane];
+        const int s = e >= ld, c = e - s * ld;
+        if (c < C) (s ? dgamma : dbeta)[c] = (float)v;
     }
 }
 
-// dgamma, dbeta: the images' rows in order, in fp64.
-__global__ void gn_finish_kernel(const float *rows, int n, int C, int ld, float *dgamma, float *dbeta)
+typedef void (*GnKernel)(GnP, GnArgs);
+
+template <int MODE>
+GnKernel gn_pick(int act, bool res)
 {
-    const int e = blockIdx.x * blockDim.x + threadIdx.x, s = e >= C, c = e - s * C;
-    if (e >= 2 * C) return;
-    double v = 0.0;
-    for (int r = 0; r < n; ++r) v += (double)rows[((size_t)r * 2 + s) * ld + c];
-    (s ? dgamma : dbeta)[c] = (float)v;
+    switch (act) {
+    case PT_ACT_NONE: return res ? gn_kernel<MODE, PT_ACT_NONE, true> : gn_kernel<MODE, PT_ACT_NONE, false>;
+    case PT_ACT_RELU: return res ? gn_kernel<MODE, PT_ACT_RELU, true> : gn_kernel<MODE, PT_ACT_RELU, false>;
+    default: return res ? gn_kernel<MODE, PT_ACT_SILU, true> : gn_kernel<MODE, PT_ACT_SILU, false>;
+    }
+}
+
+GnKernel gn_kernel_of(int mode, int act, bool res)
+{
+    switch (mode) {
+    case kGnFwd: return gn_pick<kGnFwd>(act, res);
+    case kGnFwdPack: return gn_pick<kGnFwdPack>(act, res);
+    case kGnBwd: return gn_pick<kGnBwd>(act, res);
+    default: return gn_pick<kGnBwdPacked>(act, res);
+    }
 }
 
 pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
@@ -221,7 +714,7 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     if (d->N < 1 || d->H < 1 || d->W < 1 || d->C < 1 || d->ld < d->C || (d->ld & 7)) return PT_ERR_INVALID_ARG;
     if (d->groups < 1 || d->groups > d->C || !(d->eps >= 0.f) || d->act < PT_ACT_NONE || d->act > PT_ACT_SILU) return PT_ERR_INVALID_ARG;
     if (codes && (d->ldq < d->C || (d->ldq & 7))) return PT_ERR_INVALID_ARG;
-    p->table = 0;
+    memset(p, 0, sizeof(*p));
     const int32_t *b = d->group_begin;
     if (b) {
         if (b[0] != 0 || b[d->groups] != d->C) return PT_ERR_INVALID_ARG;
@@ -238,35 +731,105 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     if (p->table)
         for (int g = 0; g <= d->groups; ++g) p->begin[g] = (uint16_t)b[g];
     p->N = d->N; p->HW = (int)hw; p->C = d->C; p->ld = d->ld; p->LV = d->ld / 8; p->ldq = d->ldq; p->nb = pt_ceil_div(d->C, act8::kBlock);
-    p->G = d->groups; p->act = d->act; p->eps = d->eps;
+    p->G = d->groups; p->eps = d->eps;
     p->w = p->LV >= 3 ? 4 : p->LV;
-    p->rl = pt_ceil_div(p->LV, p->w) * p->w;
-    p->ppb = kGnThreads / p->rl;
     return PT_OK;
 }
 
-size_t gn_smem(const GnP &p) { return kGnThreads * 16 * sizeof(float) + 2 * (size_t)p.ld * sizeof(double) + 4 * (size_t)p.ld * sizeof(float); }
+// The launch shape for clusters of cl blocks: how the threads cover a pixel row, and the shared memory's parts. Returns its bytes.
+size_t gn_shape(GnP *p, int mode, bool res, int cl)
+{
+    p->cl = cl;
+    p->share = pt_ceil_div(p->HW, cl);
+    p->rl = mode == kGnFwdPack ? pt_ceil_div(p->LV, p->w) * p->w : p->LV;
+    p->ppb = kGnThreads / p->rl;
+    if (p->ppb > p->share) p->ppb = p->share;
+    p->threads = (p->rl * p->ppb + 31) / 32 * 32;
+    p->pieces = p->threads / (16 * p->LV);
+    if (p->pieces > p->ppb) p->pieces = p->ppb;
+    if (p->pieces < 1) p->pieces = 1;
+    // lanes of a group: as many as there are for it, no more than it has channels
+    int most = pt_ceil_div(p->C, p->G);
+    if (p->table)
+        for (int g = 0; g < p->G; ++g) most = most > p->begin[g + 1] - p->begin[g] ? most : p->begin[g + 1] - p->begin[g];
+    p->gl = 1;
+    while (p->gl < 32 && p->gl < most && 2 * p->gl * p->G <= p->threads) p->gl *= 2;
+    size_t at = 0;
+    const auto part = [&](unsigned *off, size_t bytes) { *off = (unsigned)at; at += pt_align_up(bytes, 16); };
+    part(&p->sm_ring, (size_t)kGnThreads * kGnRows * gn_batches(mode, res) * gn_slot(mode, res));
+    part(&p->sm_gid, (size_t)p->ld * 2);
+    part(&p->sm_gam, (size_t)p->ld * 4);
+    part(&p->sm_bet, (size_t)p->ld * 4);
+    part(&p->sm_grp, (size_t)p->G * 6 * 4);
+    part(&p->sm_chan, (size_t)p->pieces * 16 * p->LV * 4);
+    part(&p->sm_red, (size_t)p->threads * 17 * 4);
+    part(&p->sm_xch, (size_t)2 * cl * p->G * 16);
+    part(&p->sm_acc, gn_bwd(mode) ? (size_t)2 * p->ld * 8 : 0);
+    return at;
+}
 
 bool aligned16(const void *q) { return ((uintptr_t)q & 15) == 0; }
 
-template <bool BWD>
-pt_status launch_gn(pt_ctx *c, const GnP &p, const GnArgs &a, cudaStream_t st)
+pt_status launch_gn(pt_ctx *c, GnP p, GnArgs a, int mode, int act, cudaStream_t st)
 {
-    PT_CUDA_OK(cudaFuncSetAttribute(gn_kernel<BWD>, cudaFuncAttributeMaxDynamicSharedMemorySize, 100 * 1024));
-    gn_kernel<BWD><<<p.N, kGnThreads, gn_smem(p), st>>>(p, a);
+    const bool res = a.res != nullptr;
+    const GnKernel kernel = gn_kernel_of(mode, act, res);
+    const unsigned bit = 1u << ((mode * 3 + act) * 2 + (res ? 1 : 0));
+    if (!(c->gn_attr & bit)) {
+        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024));
+        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        c->gn_attr |= bit;
+    }
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    memset(&cfg, 0, sizeof(cfg));
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    // the cluster size of the least estimated time
+    double best = 1e30;
+    int best_cl = 0, best_n = 0;
+    for (int cl = 1; cl <= kGnMaxCluster; cl *= 2) {
+        if (cl > 1 && (cl > p.HW || cl * p.G > kGnExchange)) break;
+        GnP q = p;
+        const size_t smem = gn_shape(&q, mode, res, cl);
+        if (smem > 225 * 1024) continue;
+        cfg.gridDim = dim3((unsigned)cl); cfg.blockDim = dim3((unsigned)q.threads); cfg.dynamicSmemBytes = smem;
+        attr[1].val.clusterDim.x = (unsigned)cl;
+        cfg.numAttrs = 2;
+        int n = 0;
+        if (cl > 1) {
+            PT_CUDA_OK(cudaOccupancyMaxActiveClusters(&n, (const void *)kernel, &cfg));
+        } else {
+            PT_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)kernel, (int)cfg.blockDim.x, smem));
+            n *= c->sm_count;
+        }
+        if (n < 1) continue;
+        if (n > kGnBlocks * c->sm_count) n = kGnBlocks * c->sm_count;
+        const int clusters = n < p.N ? n : p.N, waves = pt_ceil_div(p.N, clusters);
+        const double slot = gn_slot(mode, res), in = (double)q.share * p.LV * slot, ring = (double)kGnThreads * kGnRows * gn_batches(mode, res) * slot;
+        const double bytes = in + 2.0 * q.share * p.ld + 0.5 * (in > ring ? in - ring : 0.0);
+        double rate = 6500e3 / (clusters * cl);                   // bytes per microsecond and block
+        if (rate > 60e3) rate = 60e3;
+        const double us = waves * (bytes / rate + 2.0 + (cl > 1 ? 0.5 : 0.0));
+        if (us < best) { best = us; best_cl = cl; best_n = clusters; }
+    }
+    if (!best_cl) return PT_ERR_UNSUPPORTED;
+    const size_t smem = gn_shape(&p, mode, res, best_cl);
+    p.clusters = best_n;
+    cfg.gridDim = dim3((unsigned)(p.clusters * p.cl)); cfg.blockDim = dim3((unsigned)p.threads); cfg.dynamicSmemBytes = smem;
+    attr[1].val.clusterDim.x = (unsigned)p.cl;
+    cfg.numAttrs = p.cl > 1 ? 2 : 1;
+    PT_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p, a));
     c->launches += 1;
-    PT_CUDA_OK(cudaGetLastError());
-    return PT_OK;
-}
-
-pt_status gn_backward(pt_ctx *c, const GnP &p, GnArgs &a, float *dgamma, float *dbeta, void *ws, cudaStream_t st)
-{
-    a.rows = (float *)ws;
-    pt_status r = launch_gn<true>(c, p, a, st);
-    if (r != PT_OK) return r;
-    gn_finish_kernel<<<pt_ceil_div(2 * p.C, 128), 128, 0, st>>>(a.rows, p.N, p.C, p.ld, dgamma, dbeta);
-    c->launches += 1;
-    PT_CUDA_OK(cudaGetLastError());
+    if (mode >= kGnBwd && p.clusters > 1) {
+        PT_CUDA_OK(pt_launch_pdl(gn_finish_kernel, dim3((unsigned)pt_ceil_div(2 * p.ld, 32)), dim3(1024), 0, st, (const double *)a.rows, p.clusters, p.C,
+                                 p.ld, a.dgamma, a.dbeta));
+        c->launches += 1;
+    }
     return PT_OK;
 }
 
@@ -276,7 +839,9 @@ extern "C" size_t pt_gn_workspace_bytes(const pt_ctx *c, const pt_gn_desc *d)
 {
     GnP p;
     if (gn_params(c, d, false, &p) != PT_OK) return 0;
-    return (size_t)p.N * 2 * p.ld * sizeof(float);
+    // a row of sums per cluster: no more than there are images, or blocks on the device
+    const size_t most = (size_t)c->sm_count * 2;
+    return ((size_t)p.N < most ? (size_t)p.N : most) * 2 * p.ld * sizeof(double);
 }
 
 extern "C" pt_status pt_gn_act_fwd(pt_ctx *c, const pt_gn_desc *d, const void *x, const void *residual, const float *gamma, const float *beta,
@@ -290,7 +855,7 @@ extern "C" pt_status pt_gn_act_fwd(pt_ctx *c, const pt_gn_desc *d, const void *x
     GnArgs a{};
     a.x = (const uint4 *)x; a.res = (const uint4 *)residual; a.gamma = gamma; a.beta = beta; a.save_mean = save_mean; a.save_rstd = save_rstd;
     a.y = (uint4 *)y; a.codes = (uint8_t *)codes; a.scales = (uint8_t *)scales;
-    return launch_gn<false>(c, p, a, (cudaStream_t)stream);
+    return launch_gn(c, p, a, codes ? kGnFwdPack : kGnFwd, d->act, (cudaStream_t)stream);
 }
 
 extern "C" pt_status pt_gn_act_bwd(pt_ctx *c, const pt_gn_desc *d, const void *x, const void *residual, const void *dy, const float *gamma,
@@ -306,7 +871,8 @@ extern "C" pt_status pt_gn_act_bwd(pt_ctx *c, const pt_gn_desc *d, const void *x
     GnArgs a{};
     a.x = (const uint4 *)x; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy; a.gamma = gamma; a.beta = beta; a.mean = save_mean;
     a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual;
-    return gn_backward(c, p, a, dgamma, dbeta, ws, (cudaStream_t)stream);
+    a.rows = (double *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    return launch_gn(c, p, a, kGnBwd, d->act, (cudaStream_t)stream);
 }
 
 extern "C" pt_status pt_gn_act_bwd_packed(pt_ctx *c, const pt_gn_desc *d, const void *codes, const void *scales, const void *residual,
@@ -323,5 +889,6 @@ extern "C" pt_status pt_gn_act_bwd_packed(pt_ctx *c, const pt_gn_desc *d, const 
     GnArgs a{};
     a.codes_in = (const uint8_t *)codes; a.scales_in = (const uint8_t *)scales; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy;
     a.gamma = gamma; a.beta = beta; a.mean = save_mean; a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual; a.y = (uint4 *)y;
-    return gn_backward(c, p, a, dgamma, dbeta, ws, (cudaStream_t)stream);
+    a.rows = (double *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    return launch_gn(c, p, a, kGnBwdPacked, d->act, (cudaStream_t)stream);
 }

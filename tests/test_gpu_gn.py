@@ -340,12 +340,18 @@ def test_offsets_beyond_32_bits():
     torch.cuda.synchronize()
     c.poll()
     names = ("mean", "rstd", "y", "dx", "checkpoint")
-    # (the sums of one image may be split over more blocks than those of many: the last bits of its statistics differ)
+    # The sums of one image may be split over more blocks than those of many: the statistics differ by what each may be off (above). That
+    # is 2e-6 of |mean| + the standard deviation for a mean (each value's rounding is relative to the value, and they are about 1, while
+    # the means here are about 1 / sqrt(131072)), twice that between two of them, and 4e-6 twice for rstd. A bf16 result then differs by a
+    # step at most.
     for k, a, b in zip(names, whole, last):
+        off = (a.double() - b.double()).abs().max()
         if k == "checkpoint":
             assert torch.equal(a, b)
+        elif k == "mean":
+            assert float(off) <= 4e-6 * float(b.abs().max() + 1 / last[1].min())
         else:
-            assert float((a.double() - b.double()).abs().max()) <= (1e-5 if k in ("mean", "rstd") else 2.0 ** -7) * float(b.abs().max()), k
+            assert float(off) <= (8e-6 if k == "rstd" else 2.0 ** -7) * float(b.abs().max()), k
 
 
 # ------------------------------------------------------------------------------------------------ checkpoints by themselves
