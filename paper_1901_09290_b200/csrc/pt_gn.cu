@@ -775,10 +775,10 @@ pt_status launch_gn(pt_ctx *c, GnP p, GnArgs a, int mode, int act, cudaStream_t 
     const bool res = a.res != nullptr;
     const GnKernel kernel = gn_kernel_of(mode, act, res);
     const unsigned bit = 1u << ((mode * 3 + act) * 2 + (res ? 1 : 0));
-    if (!(c->gn_attr & bit)) {
+    if (!(c->gn_attr_done & bit)) {
         PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024));
         PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        c->gn_attr |= bit;
+        c->gn_attr_done |= bit;
     }
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];

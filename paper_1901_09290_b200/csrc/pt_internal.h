@@ -71,7 +71,7 @@ struct pt_ctx {
     int device = 0;
     int sm_count = 0;
     mutable std::atomic<unsigned> attr_done{0};
-    mutable std::atomic<unsigned> gn_attr{0};            // the same for the group-norm kernels
+    mutable std::atomic<unsigned> gn_attr_done{0};            // the same for the group-norm kernels
     int cc_major = 0, cc_minor = 0;
     unsigned int *d_status = nullptr;   // 4 words, device
     unsigned int *h_status = nullptr;   // 4 words, pinned host
