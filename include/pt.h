@@ -270,7 +270,7 @@ pt_status pt_bn_relu_bwd(pt_ctx *ctx, const pt_bn_desc *d, const void *x, const 
  * as an input of its call (y as x or residual; dx and dresidual as x, residual or dy, but not as each other); otherwise no two overlap.
  * An infinity or a NaN in x makes the outputs of its image and group NaN.
  * The current device must be the context's. PT_ERR_INVALID_ARG for bad sizes, pitches, alignment, groups, missing pointers or another
- * current device; PT_ERR_UNSUPPORTED for ld > 2048, H*W >= 2^31, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.
+ * current device; PT_ERR_UNSUPPORTED for ld > 2048, an image of 4 GB or more, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.
  * ------------------------------------------------------------------------------------------ */
 enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_SILU = 2 };
 typedef struct {

@@ -38,11 +38,10 @@ constexpr int kGnBlocks = 2;                 // blocks of an SM: while one excha
 struct GnP {
     int N, HW, C, ld, LV, ldq, nb, G;
     int w, rl, ppb, threads;     // lanes of a checkpoint's block, lanes of a pixel, pixels the threads cover at a time, threads
-    int pieces;                  // parts of the threads' sums of a channel that are added side by side
-    int gl;                      // lanes that add up a group
+    int gl, gc;                  // lanes that add up a group, and those of them that take different channels
     int cl, clusters, share;     // blocks of a cluster, clusters, pixels of a block
     int table;
-    unsigned sm_gid, sm_gam, sm_bet, sm_grp, sm_chan, sm_red, sm_xch, sm_acc, sm_ring;
+    unsigned sm_gid, sm_gam, sm_bet, sm_grp, sm_red, sm_xch, sm_acc, sm_ring;
     float eps;
     uint16_t begin[kGnTable + 1];
 };
@@ -80,16 +79,17 @@ __device__ __forceinline__ uint32_t to_bf(f2 x)
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
-// sigmoid of a pair, 1/(1 + exp(-z)): one reciprocal serves both, 1/a = b/(a*b), which is one of the three operations per value that go
-// through the special-function units (16 lanes a cycle: at the rate HBM brings values they are two thirds busy in the backward pass). Below
-// -40 the sigmoid is taken at -40 (4e-18), which keeps a*b finite. Off by 2 ulp and |z| * 2^-24. (A NaN does not come through: the result
-// is only ever multiplied by z.)
-__device__ __forceinline__ f2 sigmoid2(f2 z)
+// SiLU works on w = -z * log2(e), which costs nothing: the factor is in the constants that give z. sigmoid(z) = 1/(1 + 2^w), 2 ulp and
+// |z| * 2^-24 off. One reciprocal serves a pair, 1/a = b/(a*b): the special-function units take 8 cycles for an instruction of a warp, and
+// with two exponentials and two reciprocals per pair, twice in the backward pass, they were the bound at 64x56x56x256 (46 us of their time
+// alone; 35 with one reciprocal). 2^w stops at 2^60, a sigmoid of 1e-18, so that a*b is finite. (A NaN does not come through: the
+// result is only ever multiplied by w.)
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ f2 sigmoid_w(f2 w)
 {
     float a, b;
-    un2(mul2(z, mk2(-1.4426950408889634f, -1.4426950408889634f)), a, b);           // -z * log2(e)
-    const f2 e = add2(mk2(ex2(fminf(a, 57.7f)), ex2(fminf(b, 57.7f))), mk2(1.f, 1.f));
-    un2(e, a, b);
+    un2(w, a, b);
+    un2(add2(mk2(ex2(fminf(a, 60.f)), ex2(fminf(b, 60.f))), mk2(1.f, 1.f)), a, b);
     const float r = rcp(a * b);
     return mk2(r * b, r * a);
 }
@@ -98,7 +98,7 @@ template <int ACT>
 __device__ __forceinline__ f2 activate2(f2 z)
 {
     if (ACT == PT_ACT_NONE) return z;
-    if (ACT == PT_ACT_SILU) return mul2(z, sigmoid2(z));
+    if (ACT == PT_ACT_SILU) return mul2(mul2(z, mk2(-kLn2, -kLn2)), sigmoid_w(z));       // (of w)
     float a, b;
     un2(z, a, b);
     return mk2(a > 0.f ? a : (a != a ? a : 0.f), b > 0.f ? b : (b != b ? b : 0.f));
@@ -184,7 +184,6 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     float *gam = reinterpret_cast<float *>(smem + p.sm_gam), *bet = reinterpret_cast<float *>(smem + p.sm_bet);      // [ld]
     float *grps = reinterpret_cast<float *>(smem + p.sm_grp);            // [2][2][G] of alternating images: mean and rstd (backward), pivot
     float *out = grps + 4 * p.G;                                         // [2][G] rstd and mean (forward), the group's terms of dx (backward)
-    float *chan = reinterpret_cast<float *>(smem + p.sm_chan);           // [pieces][2][8 LV]
     float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][17]
     double2 *xch = reinterpret_cast<double2 *>(smem + p.sm_xch);         // [2][cl][G]
     double *acc = reinterpret_cast<double *>(smem + p.sm_acc);           // [2][ld]
@@ -192,8 +191,13 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     const int rank = (int)(blockIdx.x % p.cl), cluster = (int)(blockIdx.x / p.cl);
     const int first = rank * p.share, mine = p.HW - first < p.share ? (p.HW - first > 0 ? p.HW - first : 0) : p.share;
     const int step = U * p.ppb, NB = (mine + step - 1) / step;           // pixels and number of the block's batches
-    const int pr = t / p.rl, cv = t - pr * p.rl, c0 = cv * 8;
-    const bool lane_ok = pr < p.ppb && cv < p.LV, has = lane_ok && c0 < p.C;     // has: the vector holds channels, not pad lanes only
+    // Threads without a vector of their own (t >= rl * ppb, or lanes that only fill up a checkpoint's block) do what thread 0 does and store
+    // nothing. Vectors of pad lanes only are read and come out as zeros; their codes, which there are none of, are read as vector 0's.
+    int pr = t / p.rl, cv = t - pr * p.rl;
+    const bool lane_ok = pr < p.ppb && cv < p.LV;
+    if (!lane_ok) pr = cv = 0;
+    const int c0 = cv * 8;
+    const bool has = c0 < p.C;                                           // the vector holds channels, not pad lanes only
     const uint4 keep = act8::keep_bits(c0, p.C);
     const uint8_t *mine_x = smem + p.sm_ring + t * kXs, *mine_v = smem + p.sm_ring + t * 16, *mine_s = smem + p.sm_ring + kSc + t * 4;
     const uint32_t to_x = sm100::smem_u32(mine_x), to_v = sm100::smem_u32(mine_v), to_s = sm100::smem_u32(mine_s);
@@ -202,49 +206,80 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     for (int c = p.C + t; c < p.ld; c += p.threads) gid[c] = (uint16_t)(p.G - 1);
     sm100::grid_dependency_wait();
     sm100::grid_launch_dependents();
-    // batch b of image n into the ring's place s
-    const auto bring = [&](int n, int b, int s) {
-        if (has && n < p.N && b < NB) {
-            const int r0 = b * step + pr;
-            const size_t pix0 = (size_t)n * p.HW + first;
+    // Offsets in bytes from an image's first pixel of this block: 32 bits, added to addresses that all threads share.
+    const uint32_t row = (uint32_t)p.ld * 2u, step_v = (uint32_t)step * row, step_q = (uint32_t)(step * p.ldq), step_s = (uint32_t)(step * p.nb);
+    uint32_t off[U], off_q[U], off_s[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int r = r0 + u * p.ppb;
-                if (r < mine) {
-                    const size_t pix = pix0 + r, at = pix * p.LV + cv;
-                    if (PACKED) {
-                        const size_t sc = pix * p.nb + (cv >> 2);
-                        copy8(to_x + (uint32_t)(s * U + u) * kRowX, a.codes_in + pix * p.ldq + c0);
-                        copy4(to_s + (uint32_t)(s * U + u) * kRowS, a.scales_in + (sc & ~(size_t)3));
-                    } else {
-                        copy16(to_x + (uint32_t)(s * U + u) * kRowX, a.x + at);
-                    }
-                    if (BWD) copy16(to_v + kDy + (uint32_t)(s * U + u) * kRow, a.dy + at);
-                    if (BWD && RES) copy16(to_v + kRes + (uint32_t)(s * U + u) * kRow, a.res + at);
-                }
-            }
-        }
-        copy_commit();
+    for (int u = 0; u < U; ++u) {
+        const uint32_t r = (uint32_t)(pr + u * p.ppb);
+        off[u] = r * row + (uint32_t)cv * 16u;
+        off_q[u] = r * (uint32_t)p.ldq + (has ? (uint32_t)c0 : 0u);
+        off_s[u] = r * (uint32_t)p.nb + (has ? (uint32_t)(cv >> 2) : 0u);
+    }
+    const auto bytes = [](const void *q) { return reinterpret_cast<const uint8_t *>(q); };
+    struct Src { const uint8_t *x, *dy, *res, *q, *s; };                 // an image's tensors from the block's first pixel on
+    const auto source = [&](int n) {
+        Src g{};
+        const size_t pix = (size_t)n * p.HW + first;
+        if (PACKED) { g.q = a.codes_in + pix * p.ldq; g.s = a.scales_in + pix * p.nb; }
+        else g.x = bytes(a.x) + pix * row;
+        if (BWD) g.dy = bytes(a.dy) + pix * row;
+        if (RES) g.res = bytes(a.res) + pix * row;
+        return g;
     };
-#pragma unroll 1
-    for (int b = 0; b < B; ++b) bring(cluster, b, b);
+    // batch b of an image into the ring's place s (a multiple of U)
+    const auto bring = [&](const Src &g, int b, int s) {
+        const uint32_t bv = (uint32_t)b * step_v, bq = (uint32_t)b * step_q, bs = (uint32_t)b * step_s;
+        const auto one = [&](int u) {
+            if (PACKED) {
+                copy8(to_x + (uint32_t)(s + u) * kRowX, g.q + (bq + off_q[u]));
+                copy4(to_s + (uint32_t)(s + u) * kRowS, reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(g.s + (bs + off_s[u])) & ~(uintptr_t)3));
+            } else {
+                copy16(to_x + (uint32_t)(s + u) * kRowX, g.x + (bv + off[u]));
+            }
+            if (BWD) copy16(to_v + kDy + (uint32_t)(s + u) * kRow, g.dy + (bv + off[u]));
+            if (BWD && RES) copy16(to_v + kRes + (uint32_t)(s + u) * kRow, g.res + (bv + off[u]));
+        };
+        if ((b + 1) * step <= mine) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) one(u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (b * step + u * p.ppb + pr < mine) one(u);
+        }
+    };
+    // (these loads first: behind the ring's copies they would wait for those)
+    const bool ahead = BWD && p.G <= p.threads;                          // an image's statistics are fetched before they are needed
+    float next_mean = 0.f, next_rstd = 0.f;
+    if (ahead && t < p.G) {
+        next_mean = a.mean[(size_t)cluster * p.G + t];
+        next_rstd = a.rstd[(size_t)cluster * p.G + t];
+    }
     for (int c = t; c < p.ld; c += p.threads) {
         gam[c] = c < p.C ? a.gamma[c] : 0.f;
-        bet[c] = c < p.C ? a.beta[c] : 0.f;
+        bet[c] = c < p.C ? a.beta[c] : 1.f;                              // (a pad lane's z must not be near 0, see gradient)
         if (BWD) acc[c] = acc[p.ld + c] = 0.0;
+    }
+    Src src = source(cluster);
+#pragma unroll 1
+    for (int b = 0; b < B; ++b) {
+        if (b < NB) bring(src, b, b * U);
+        copy_commit();
     }
     int dir = 0, it = 0;
     const double inv_hw = 1.0 / (double)p.HW;
-    const bool ahead = BWD && p.G <= p.threads;                          // the next image's statistics are fetched during the second walk
-    float next_mean = 0.f, next_rstd = 0.f;
+    const int whole = p.HW / p.share;                                    // blocks with all their pixels
+    const double rest = (double)(p.HW - whole * p.share);                // pixels of the one behind them
     for (int n = cluster; n < p.N; n += p.clusters, dir ^= 1, ++it) {
         const size_t base = (size_t)n * p.HW + first;                    // the block's first pixel
+        const Src next = source(n + p.clusters < p.N ? n + p.clusters : n);
         // (so that a batch of the first walk always has B - 1 groups behind it when it is waited for)
         if (it > 0)
             for (int b = NB; b < B; ++b) copy_commit();
         // ---- what the first walk needs of every group: the statistics (backward), or a value near its mean (forward)
         float *grp = grps + (it & 1) * 2 * p.G;
-        if (BWD && ahead && it > 0) {
+        if (BWD && ahead) {
             if (t < p.G) { grp[t] = next_mean; grp[p.G + t] = next_rstd; }
         } else if (BWD) {
             for (int g = t; g < p.G; g += p.threads) {
@@ -271,19 +306,20 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         __syncthreads();
         // the thread's constants: minus the mean (or pivot), and in the backward pass gamma*rstd, beta, and the ReLU's limits as bf16: without
         // a residual, z > 0 exactly where x ^ sgn > thr
-        f2 nm[4], k[4], be[4];
+        f2 nm[4], k[4], kz[4], be[4];                                    // (kz: k, or for SiLU what gives w)
         uint32_t thr[4], sgn[4];
-        float be_max = 0.f;
+        float be_max = 1e-30f;                                           // (z so small that bf16 might not hold it is decided there too)
         {
             float m[8], kk[8], b[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = has ? c0 + j : 0, g = gid[c];
+                const int c = c0 + j, g = gid[c];
                 m[j] = -grp[g];
                 if (BWD) {
                     kk[j] = gam[c] * grp[p.G + g];
                     b[j] = bet[c];
-                    be_max = fmaxf(be_max, fabsf(b[j]));
+                    be_max = fmaxf(be_max, 1e-6f * fabsf(b[j]));
+                    if (ACT == PT_ACT_SILU) b[j] *= -kLog2e;
                 }
                 if (BWD && ACT == PT_ACT_RELU && !RES) {
                     // z = s*(x - mean) + beta > 0  <=>  x > mean - beta/s (s > 0), -x > -(mean - beta/s) (s < 0); a constant for s = 0
@@ -297,20 +333,25 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 nm[i] = mk2(m[2 * i], m[2 * i + 1]);
-                if (BWD) { k[i] = mk2(kk[2 * i], kk[2 * i + 1]); be[i] = mk2(b[2 * i], b[2 * i + 1]); }
+                if (BWD) {
+                    k[i] = mk2(kk[2 * i], kk[2 * i + 1]);
+                    kz[i] = ACT == PT_ACT_SILU ? mul2(k[i], mk2(-kLog2e, -kLog2e)) : k[i];
+                    be[i] = mk2(b[2 * i], b[2 * i + 1]);
+                }
             }
         }
-        // pixel u of the batch at the ring's place s; r: its number among the block's pixels
-        const auto fetch = [&](Raw &w, int s, int u, int r) {
+        // pixel u of a batch, at the ring's place s; bs: the batch's offset in the scales
+        const uint32_t s_base = PACKED ? (uint32_t)(base * p.nb) : 0u;   // (the buffer starts on a word)
+        const auto fetch = [&](Raw &w, uint32_t bs, int s, int u) {
             if (PACKED) {
-                w.q = *reinterpret_cast<const uint2 *>(mine_x + (uint32_t)(s * U + u) * kRowX);
-                const uint32_t sc = (uint32_t)((base + r) * p.nb) + (uint32_t)(cv >> 2);
-                w.byte = *reinterpret_cast<const uint32_t *>(mine_s + (uint32_t)(s * U + u) * kRowS) >> ((sc & 3u) * 8u) & 0xffu;
+                w.q = *reinterpret_cast<const uint2 *>(mine_x + (uint32_t)(s + u) * kRowX);
+                const uint32_t sc = s_base + bs + off_s[u];
+                w.byte = *reinterpret_cast<const uint32_t *>(mine_s + (uint32_t)(s + u) * kRowS) >> ((sc & 3u) * 8u) & 0xffu;
             } else {
-                w.x = *reinterpret_cast<const uint4 *>(mine_x + (uint32_t)(s * U + u) * kRowX);
+                w.x = *reinterpret_cast<const uint4 *>(mine_x + (uint32_t)(s + u) * kRowX);
             }
-            if (BWD) w.dy = *reinterpret_cast<const uint4 *>(mine_v + kDy + (uint32_t)(s * U + u) * kRow);
-            if (BWD && RES) w.res = *reinterpret_cast<const uint4 *>(mine_v + kRes + (uint32_t)(s * U + u) * kRow);
+            if (BWD) w.dy = *reinterpret_cast<const uint4 *>(mine_v + kDy + (uint32_t)(s + u) * kRow);
+            if (BWD && RES) w.res = *reinterpret_cast<const uint4 *>(mine_v + kRes + (uint32_t)(s + u) * kRow);
         };
         const auto values = [&](Raw &w, f2 (&x)[4]) {                   // x as fp32 pairs (and, from codes, as bf16 words)
             if (PACKED) {
@@ -327,8 +368,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             if (ACT == PT_ACT_SILU || want_z || (ACT == PT_ACT_RELU && RES))
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    z[i] = fma2(d[i], k[i], be[i]);
-                    if (RES) z[i] = add2(z[i], from_bf(rb[i]));
+                    z[i] = fma2(d[i], kz[i], be[i]);
+                    if (RES) z[i] = ACT == PT_ACT_SILU ? fma2(from_bf(rb[i]), mk2(-kLog2e, -kLog2e), z[i]) : add2(z[i], from_bf(rb[i]));
                 }
             if (ACT == PT_ACT_RELU && !RES) {
 #pragma unroll
@@ -349,7 +390,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     top = __vmaxu2(top, rb[i] & 0x7fff7fffu);
                 }
                 const float rmax = fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u));
-                if (low <= 1e-6f * (rmax + be_max)) {
+                if (low <= fmaf(rmax, 1e-6f, be_max)) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // (gamma = 0, a pruned channel's or a pad lane's: z = beta + residual, of the right sign in fp32)
@@ -359,20 +400,23 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                         const bool near0 = k0 != 0.f && fabsf(zz[2 * i]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] << 16)) + fabsf(b0));
                         const bool near1 = k1 != 0.f && fabsf(zz[2 * i + 1]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] & 0xffff0000u)) + fabsf(b1));
                         uint32_t m = (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
-                        if (near0 || near1) m = exact_mask(xb[i], rb[i], (has ? c0 : 0) + 2 * i, gid, grp, p.G, gam, bet);
+                        if (near0 || near1) m = exact_mask(xb[i], rb[i], c0 + 2 * i, gid, grp, p.G, gam, bet);
                         g[i] &= m;
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) g[i] &= (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
+                    for (int i = 0; i < 4; ++i) {                        // (the sign is that of z as bf16)
+                        const uint32_t u = to_bf(z[i]), zero = 0u;
+                        g[i] &= __hgt2_mask(*reinterpret_cast<const __nv_bfloat162 *>(&u), *reinterpret_cast<const __nv_bfloat162 *>(&zero));
+                    }
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 dz[i] = from_bf(g[i]);
-                if (ACT == PT_ACT_SILU) {                                // act' = s + z*s*(1 - s)
-                    const f2 s = sigmoid2(z[i]);
-                    dz[i] = mul2(dz[i], fma2(mul2(z[i], s), fma2(s, mk2(-1.f, -1.f), mk2(1.f, 1.f)), s));
+                if (ACT == PT_ACT_SILU) {                                // act' = s + z*s*(1 - s) = s * (1 + w * ln 2 * (s - 1))
+                    const f2 s = sigmoid_w(z[i]);
+                    dz[i] = mul2(mul2(dz[i], s), fma2(z[i], fma2(s, mk2(kLn2, kLn2), mk2(-kLn2, -kLn2)), mk2(1.f, 1.f)));
                 }
             }
         };
@@ -411,89 +455,77 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             }
             flushed = true;
         };
-        int s = dir ? B - 1 : 0;
+        // the ring's places in the order of the walk, and where they begin and end
+        const int s_first = dir ? (B - 1) * U : 0, s_last = dir ? 0 : (B - 1) * U, s_step = dir ? -U : U;
+        int s = s_first;
         for (int b = 0; b < NB; ++b) {
             copy_wait<B - 1>();
-            const int r0 = b * step + pr;
+            const int left = mine - b * step - pr;                       // pixel u is there if u * ppb < left
+            const uint32_t bs = (uint32_t)b * step_s;
             if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
+                uint8_t *gq = a.codes + base * p.ldq, *gs = a.scales + base * p.nb;
+                const uint32_t bq = (uint32_t)b * step_q;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int r = r0 + u * p.ppb;
-                    const bool ok = has && r < mine;
+                    const bool ok = u * p.ppb < left;
                     Raw w;
                     w.x = make_uint4(0u, 0u, 0u, 0u);
                     if (ok) {
-                        fetch(w, s, u, r);
+                        fetch(w, bs, s, u);
                         count(w);
                     }
                     w.x = act8::and4(w.x, keep);
+                    if (!lane_ok) w.x = make_uint4(0u, 0u, 0u, 0u);
                     const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(w.x), p.w));
-                    if (ok) {
-                        *reinterpret_cast<uint2 *>(a.codes + (base + r) * p.ldq + c0) = act8::encode8(w.x, byte);
-                        if ((cv & 3) == 0) a.scales[(base + r) * p.nb + (cv >> 2)] = (uint8_t)byte;
+                    if (ok && lane_ok && has) {
+                        *reinterpret_cast<uint2 *>(gq + (bq + off_q[u])) = act8::encode8(w.x, byte);
+                        if ((cv & 3) == 0) gs[bs + off_s[u]] = (uint8_t)byte;
                     }
                 }
-            } else if (has) {
-                if ((b + 1) * step <= mine) {                            // two pixels at a time, their loads first
-                    Raw w[U];
+            } else if ((b + 1) * step <= mine) {                         // two pixels at a time, their loads first
+                Raw w[U];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) fetch(w[u], s, u, r0 + u * p.ppb);
+                for (int u = 0; u < U; ++u) fetch(w[u], bs, s, u);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) count(w[u]);
-                } else {
-#pragma unroll 1
-                    for (int u = 0; u < U; ++u)
-                        if (r0 + u * p.ppb < mine) {
-                            Raw w;
-                            fetch(w, s, u, r0 + u * p.ppb);
-                            count(w);
-                        }
-                }
+                for (int u = 0; u < U; ++u) count(w[u]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (u * p.ppb < left) {
+                        Raw w;
+                        fetch(w, bs, s, u);
+                        count(w);
+                    }
             }
-            if (b + B < NB) bring(n, b + B, s);                          // (the last B batches stay for the second walk)
-            else copy_commit();
+            if (b + B < NB) bring(src, b + B, s);                        // (the last B batches stay for the second walk)
+            copy_commit();
             if ((b & 31) == 31 || b == NB - 1) flush();
-            if (dir) s = s == 0 ? B - 1 : s - 1;
-            else s = s == B - 1 ? 0 : s + 1;
+            s = s == s_last ? s_first : s + s_step;
         }
         if (NB == 0) flush();
-        // ---- a channel's sums over the threads' rows, then a group's over its channels
+        // ---- a group's sums over the threads' rows and its channels
         __syncthreads();
-        const int cols = p.LV * 8;
-        for (int e = t; e < 2 * cols * p.pieces; e += p.threads) {
-            const int piece = e / (2 * cols), v = e - piece * 2 * cols, s = v >= cols ? 1 : 0, c = v - s * cols;
-            const float *src = red + (c >> 3) * 17 + s * 8 + (c & 7);
-            float u0 = 0.f, u1 = 0.f;
-            int r = piece;
-            for (; r + p.pieces < p.ppb; r += 2 * p.pieces) { u0 += src[r * p.rl * 17]; u1 += src[(r + p.pieces) * p.rl * 17]; }
-            if (r < p.ppb) u0 += src[r * p.rl * 17];
-            chan[e] = u0 + u1;
-        }
-        __syncthreads();
-        if (BWD)
-            for (int c = t; c < p.C; c += p.threads) {                 // the images' sums of dz and dz * xhat
-                double v0 = 0.0, v1 = 0.0;
-                for (int k = 0; k < p.pieces; ++k) { v0 += (double)chan[k * 2 * cols + c]; v1 += (double)chan[k * 2 * cols + cols + c]; }
-                acc[c] += v0;
-                acc[p.ld + c] += v1 * (double)grp[p.G + gid[c]];
-            }
         {
-            const int per = 32 / p.gl, l = lane & (p.gl - 1), buf = it & 1;
+            // a group's lanes: gc of them take its channels, the others more of the threads' rows
+            const int per = 32 / p.gl, l = lane & (p.gl - 1), lc = l & (p.gc - 1), lr = l / p.gc, nr = p.gl / p.gc, buf = it & 1;
             for (int g0 = warp * per; g0 < p.G; g0 += warps * per) {
                 const int g = g0 + lane / p.gl;
                 const int b = g < p.G ? group_begin(p, g) : 0, e = g < p.G ? group_begin(p, g + 1) : 0;
-                double v0 = 0.0, v1 = 0.0;
-                for (int c = b + l; c < e; c += p.gl) {
-                    double w0 = 0.0, w1 = 0.0;
-                    for (int k = 0; k < p.pieces; ++k) { w0 += (double)chan[k * 2 * cols + c]; w1 += (double)chan[k * 2 * cols + cols + c]; }
-                    const double f = BWD ? (double)gam[c] : 1.0;
-                    v0 += f * w0;
-                    v1 += f * w1;
+                float f0 = 0.f, f1 = 0.f;
+                for (int c = b + lc; c < e; c += p.gc) {
+                    const float *src = red + (lr * p.rl + (c >> 3)) * 17 + (c & 7);
+                    float w0 = 0.f, w1 = 0.f;
+#pragma unroll 4
+                    for (int r = lr; r < p.ppb; r += nr, src += nr * p.rl * 17) { w0 += src[0]; w1 += src[8]; }
+                    const float f = BWD ? gam[c] : 1.f;
+                    f0 = fmaf(f, w0, f0);
+                    f1 = fmaf(f, w1, f1);
                 }
                 for (int o = p.gl >> 1; o; o >>= 1) {
-                    v0 += __shfl_xor_sync(0xffffffffu, v0, o);
-                    v1 += __shfl_xor_sync(0xffffffffu, v1, o);
+                    f0 += __shfl_xor_sync(0xffffffffu, f0, o);
+                    f1 += __shfl_xor_sync(0xffffffffu, f1, o);
                 }
+                double v0 = (double)f0, v1 = (double)f1;
                 if (!BWD) {                                              // the block's mean and sum of squares about it
                     const double cnt = (double)mine * (double)(e - b), d = cnt > 0.0 ? v0 / cnt : 0.0;
                     v1 = v1 - v0 * d;
@@ -518,15 +550,23 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 if (BWD) {
                     for (int r = 0; r < p.cl; ++r) { v0 += v[(size_t)r * p.G].x; v1 += v[(size_t)r * p.G].y; }
                     const double rs = (double)grp[p.G + g], im = 1.0 / m;
-                    out[g] = -(float)(rs * v0 * im);
-                    out[p.G + g] = -(float)(rs * rs * rs * v1 * im);
+                    const double t1 = -(rs * rs * rs * v1 * im);
+                    out[g] = (float)(-(rs * v0 * im) - t1 * (double)grp[g]);
+                    out[p.G + g] = (float)t1;
                 } else {
-                    const auto cnt = [&](int r) { const int c = p.HW - r * p.share; return (double)(c < 0 ? 0 : c < p.share ? c : p.share); };
-                    for (int r = 0; r < p.cl; ++r) v0 += v[(size_t)r * p.G].x * (cnt(r) * inv_hw);
-                    for (int r = 0; r < p.cl; ++r) {
+                    // all blocks but the last have `share` pixels (those behind the last have none, and sent zeros)
+                    for (int r = 0; r < whole; ++r) v0 += v[(size_t)r * p.G].x;
+                    const double last = rest > 0.0 ? v[(size_t)whole * p.G].x : 0.0;
+                    v0 = (v0 * (double)p.share + last * rest) * inv_hw;
+                    double spread = 0.0;
+                    for (int r = 0; r < whole; ++r) {
                         const double d = v[(size_t)r * p.G].x - v0;
-                        v1 += v[(size_t)r * p.G].y + d * d * (cnt(r) * (double)size);
+                        spread += d * d;
+                        v1 += v[(size_t)r * p.G].y;
                     }
+                    spread = spread * (double)p.share + (last - v0) * (last - v0) * rest;
+                    if (rest > 0.0) v1 += v[(size_t)whole * p.G].y;
+                    v1 += spread * (double)size;
                     const float fm = (float)v0, fr = (float)rsqrt(v1 / m + (double)p.eps);
                     out[g] = fr;
                     out[p.G + g] = fm;
@@ -538,26 +578,29 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             }
         }
         __syncthreads();
-        // the second walk's constants: forward, minus the mean, gamma*rstd and beta; backward, the group's terms of dx
+        // The second walk's constants, about x itself: forward, z = x*c1 + c2; backward, z = x*kz + be and the group's terms of dx,
+        // x*c2 + c1. (What x - mean would keep of the last bits is lost in the rounding to bf16: with a mean of r standard deviations z is off by
+        // r * 2^-23, and bf16 values of one mean and 2^-8 of it apart have r < 2^8 or so.)
         f2 c1[4], c2[4];
         {
-            float u[8], v[8], m[8];
+            float u[8], v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = has ? c0 + j : 0, g = gid[c];
+                const int c = c0 + j, g = gid[c];
                 u[j] = out[g];
                 v[j] = out[p.G + g];
                 if (!BWD) {
-                    m[j] = -v[j];
+                    const float mean = v[j];
                     u[j] *= gam[c];
-                    v[j] = bet[c];
+                    v[j] = fmaf(-mean, u[j], bet[c]);
+                    if (ACT == PT_ACT_SILU) { u[j] *= -kLog2e; v[j] *= -kLog2e; }
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 c1[i] = mk2(u[2 * i], u[2 * i + 1]);
                 c2[i] = mk2(v[2 * i], v[2 * i + 1]);
-                if (!BWD) nm[i] = mk2(m[2 * i], m[2 * i + 1]);
+                if (BWD && !(ACT == PT_ACT_RELU && RES)) be[i] = fma2(nm[i], kz[i], be[i]);
             }
         }
         if (ahead && t < p.G && n + p.clusters < p.N) {
@@ -566,86 +609,94 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         }
         // ---- second walk, backwards: the results
         const bool want_y = !BWD || (PACKED && a.y);
-        const auto result = [&](Raw &w, const size_t at) {
+        // gx, gr, gy: the batch's first pixel in dx, dresidual and y
+        const auto result = [&](Raw &w, uint8_t *gx, uint8_t *gr, uint8_t *gy, uint32_t at) {
             f2 x[4], z[4], dz[4];
             uint4 o;
             uint32_t *ow = reinterpret_cast<uint32_t *>(&o);
             values(w, x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = add2(x[i], nm[i]);
             if (!BWD) {
                 const uint32_t *rb = reinterpret_cast<const uint32_t *>(&w.res);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 y = fma2(x[i], c1[i], c2[i]);
-                    if (RES) y = add2(y, from_bf(rb[i]));
+                    if (RES) y = ACT == PT_ACT_SILU ? fma2(from_bf(rb[i]), mk2(-kLog2e, -kLog2e), y) : add2(y, from_bf(rb[i]));
                     ow[i] = to_bf(activate2<ACT>(y));
                 }
-                a.y[at] = act8::and4(o, keep);
+                if (lane_ok) *reinterpret_cast<uint4 *>(gy + at) = act8::and4(o, keep);
             } else {
-                gradient(w, x, z, dz, want_y);
+                f2 d[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[i] = ACT == PT_ACT_RELU && RES ? add2(x[i], nm[i]) : x[i];
+                gradient(w, d, z, dz, want_y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ow[i] = to_bf(fma2(k[i], dz[i], fma2(x[i], c2[i], c1[i])));
-                a.dx[at] = act8::and4(o, keep);
+                if (lane_ok) *reinterpret_cast<uint4 *>(gx + at) = act8::and4(o, keep);
                 if (a.dres) {
                     if (ACT == PT_ACT_SILU) w.dy = make_uint4(to_bf(dz[0]), to_bf(dz[1]), to_bf(dz[2]), to_bf(dz[3]));
-                    a.dres[at] = act8::and4(w.dy, keep);
+                    if (lane_ok) *reinterpret_cast<uint4 *>(gr + at) = act8::and4(w.dy, keep);
                 }
                 if (want_y) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) ow[i] = to_bf(activate2<ACT>(z[i]));
-                    a.y[at] = act8::and4(o, keep);
+                    if (lane_ok) *reinterpret_cast<uint4 *>(gy + at) = act8::and4(o, keep);
                 }
             }
         };
         Raw ahead_w[U];                                                  // forward: the residual, a batch ahead
         const auto residual = [&](int b) {
-            if (!BWD && RES && has && b >= 0)
+            if (!BWD && RES && b >= 0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int r = b * step + u * p.ppb + pr;
-                    if (r < mine) ahead_w[u].res = a.res[(base + r) * p.LV + cv];
-                }
+                for (int u = 0; u < U; ++u)
+                    if (b * step + u * p.ppb + pr < mine) ahead_w[u].res = *reinterpret_cast<const uint4 *>(src.res + ((uint32_t)b * step_v + off[u]));
+            }
         };
         residual(NB - 1);
-        const int keep_b = NB < B ? NB : B;
+        const int kept = NB < B ? NB : B;
+        uint8_t *gx = reinterpret_cast<uint8_t *>(a.dx) + base * row, *gr = reinterpret_cast<uint8_t *>(a.dres) + base * row, *gy = reinterpret_cast<uint8_t *>(a.y) + base * row;
         for (int b = NB - 1; b >= 0; --b) {
-            if (dir) s = s == B - 1 ? 0 : s + 1;
-            else s = s == 0 ? B - 1 : s - 1;
+            s = s == s_first ? s_last : s - s_step;
             copy_wait<B - 1>();
-            const int r0 = b * step + pr;
+            const int left = mine - b * step - pr;
+            const uint32_t bv = (uint32_t)b * step_v, bs = (uint32_t)b * step_s;
             Raw w[U];
             if (!BWD && RES) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) w[u].res = ahead_w[u].res;
                 residual(b - 1);
             }
-            if (has) {
-                if ((b + 1) * step <= mine) {
+            if ((b + 1) * step <= mine) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) fetch(w[u], s, u, r0 + u * p.ppb);
+                for (int u = 0; u < U; ++u) fetch(w[u], bs, s, u);
 #pragma unroll
-                    for (int u = 0; u < U; ++u) result(w[u], (base + r0 + u * p.ppb) * p.LV + cv);
-                } else {
+                for (int u = 0; u < U; ++u) result(w[u], gx, gr, gy, bv + off[u]);
+            } else {
 #pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (r0 + u * p.ppb < mine) {
-                            fetch(w[u], s, u, r0 + u * p.ppb);
-                            result(w[u], (base + r0 + u * p.ppb) * p.LV + cv);
-                        }
-                }
-            } else if (lane_ok) {                                        // vectors of pad lanes only
-                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-                for (int u = 0; u < U; ++u) {
-                    if (r0 + u * p.ppb >= mine) continue;
-                    const size_t at = (base + r0 + u * p.ppb) * p.LV + cv;
-                    if (BWD) { a.dx[at] = zero; if (a.dres) a.dres[at] = zero; }
-                    if (want_y) a.y[at] = zero;
-                }
+                for (int u = 0; u < U; ++u)
+                    if (u * p.ppb < left) {
+                        fetch(w[u], bs, s, u);
+                        result(w[u], gx, gr, gy, bv + off[u]);
+                    }
             }
-            if (b >= B) bring(n, b - B, s);
-            else bring(n + p.clusters, keep_b - 1 - b, dir ? keep_b - 1 - b : B - keep_b + b);
+            // the place takes an earlier batch, or one of the cluster's next image: its first goes to the place that is free first
+            if (b >= B) bring(src, b - B, s);
+            else if (n + p.clusters < p.N) bring(next, kept - 1 - b, dir ? (kept - 1 - b) * U : (B - kept + b) * U);
+            copy_commit();
         }
+        src = next;
+        if (BWD)                                                         // the images' sums of dz and dz * xhat, a channel's
+            for (int c = t; c < p.C; c += p.threads) {
+                const float *src = red + (c >> 3) * 17 + (c & 7);
+                float v0 = 0.f, v1 = 0.f, u0 = 0.f, u1 = 0.f;
+                int r = 0;
+                for (; r + 1 < p.ppb; r += 2, src += 2 * p.rl * 17) {
+                    v0 += src[0]; v1 += src[8];
+                    u0 += src[p.rl * 17]; u1 += src[p.rl * 17 + 8];
+                }
+                if (r < p.ppb) { v0 += src[0]; v1 += src[8]; }
+                acc[c] += (double)v0 + (double)u0;
+                acc[p.ld + c] += ((double)v1 + (double)u1) * (double)grp[p.G + gid[c]];
+            }
     }
     // ---- the cluster's sums over its images
     if (BWD) {
@@ -727,7 +778,7 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     }
     if (d->ld > kGnMaxLd || (p->table && d->groups > kGnTable)) return PT_ERR_UNSUPPORTED;
     const long long hw = (long long)d->H * d->W;
-    if (hw > 0x7fffffffll) return PT_ERR_UNSUPPORTED;
+    if (hw * d->ld * 2 >= 0x100000000ll || (codes && hw * d->ldq >= 0x100000000ll)) return PT_ERR_UNSUPPORTED;    // (offsets in an image have 32 bits)
     if (p->table)
         for (int g = 0; g <= d->groups; ++g) p->begin[g] = (uint16_t)b[g];
     p->N = d->N; p->HW = (int)hw; p->C = d->C; p->ld = d->ld; p->LV = d->ld / 8; p->ldq = d->ldq; p->nb = pt_ceil_div(d->C, act8::kBlock);
@@ -745,15 +796,14 @@ size_t gn_shape(GnP *p, int mode, bool res, int cl)
     p->ppb = kGnThreads / p->rl;
     if (p->ppb > p->share) p->ppb = p->share;
     p->threads = (p->rl * p->ppb + 31) / 32 * 32;
-    p->pieces = p->threads / (16 * p->LV);
-    if (p->pieces > p->ppb) p->pieces = p->ppb;
-    if (p->pieces < 1) p->pieces = 1;
-    // lanes of a group: as many as there are for it, no more than it has channels
+    // lanes of a group: as many as there are for it; as many of them for its channels as it has
     int most = pt_ceil_div(p->C, p->G);
     if (p->table)
         for (int g = 0; g < p->G; ++g) most = most > p->begin[g + 1] - p->begin[g] ? most : p->begin[g + 1] - p->begin[g];
     p->gl = 1;
-    while (p->gl < 32 && p->gl < most && 2 * p->gl * p->G <= p->threads) p->gl *= 2;
+    while (p->gl < 32 && 2 * p->gl * p->G <= p->threads && p->gl < most * p->ppb) p->gl *= 2;
+    p->gc = 1;
+    while (p->gc < p->gl && p->gc < most) p->gc *= 2;
     size_t at = 0;
     const auto part = [&](unsigned *off, size_t bytes) { *off = (unsigned)at; at += pt_align_up(bytes, 16); };
     part(&p->sm_ring, (size_t)kGnThreads * kGnRows * gn_batches(mode, res) * gn_slot(mode, res));
@@ -761,7 +811,6 @@ size_t gn_shape(GnP *p, int mode, bool res, int cl)
     part(&p->sm_gam, (size_t)p->ld * 4);
     part(&p->sm_bet, (size_t)p->ld * 4);
     part(&p->sm_grp, (size_t)p->G * 6 * 4);
-    part(&p->sm_chan, (size_t)p->pieces * 16 * p->LV * 4);
     part(&p->sm_red, (size_t)p->threads * 17 * 4);
     part(&p->sm_xch, (size_t)2 * cl * p->G * 16);
     part(&p->sm_acc, gn_bwd(mode) ? (size_t)2 * p->ld * 8 : 0);
