@@ -1,52 +1,94 @@
 // 8-bit activation checkpoints of whole tensors: bf16 [npix][ld] -> codes int8 [npix][ldq] and scale bytes [npix][ceil(C / 32)], and back.
-// Bound by memory: 3 + 1/32 bytes per value in either direction. A thread owns a 16-byte vector of a pixel; the (at most four) neighbouring
-// lanes of a block find its largest magnitude by shuffles.
+// Bound by memory: 3 + 1/32 bytes per value in either direction. A thread owns a 16-byte vector column and every so many-th pixel, four of
+// them at a time, all loads before the first use: the pair of passes takes 53.8 us at 64x56x56x256 (5.8 TB/s, 0.88 of the copy rate), and took
+// 73 with one at a time, what was in flight being the bound. The (at most four) neighbouring lanes of a block find its largest magnitude by shuffles.
 #include "pt_internal.h"
 #include "pt_act.cuh"
+#include "pt_sm100_ptx.cuh"
 
 namespace {
 
 constexpr int kPackThreads = 256;
 
+constexpr int kPackBlocks = 6;      // thread blocks of an SM at a time
+
 struct PackP {
     long long npix;
     int C, ld, ldq, LV, nb;
-    int w, rl, rows;            // lanes of a block (1, 2 or 4), lanes of a pixel (LV rounded up to w), pixels a thread block covers at a time
+    int w, rl, rows;            // lanes of a block (1, 2 or 4), lanes of a pixel, pixels a thread block covers at a time
 };
 
-__global__ void __launch_bounds__(kPackThreads) pack_kernel(const PackP p, const uint4 *x, uint8_t *codes, uint8_t *scales)
+// PACK: x -> codes, scales; otherwise back, with zeros for the pad lanes (every vector of a pixel has a lane then).
+// U: pixels of a thread at a time.
+template <bool PACK, int U>
+__global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(const PackP p, uint8_t *x, uint8_t *codes, uint8_t *scales)
 {
     const int t = threadIdx.x, pr = t / p.rl, cv = t - pr * p.rl;
-    const bool lane_ok = pr < p.rows && cv < p.LV;
-    const uint4 keep = act8::keep_bits(cv * 8, p.C);
-    for (long long p0 = (long long)blockIdx.x * p.rows; p0 < p.npix; p0 += (long long)gridDim.x * p.rows) {
-        const long long pix = p0 + pr;
-        const bool ok = lane_ok && pix < p.npix;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (ok) v = act8::and4(x[pix * (p.ld / 8) + cv], keep);
-        const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(v), p.w));
-        if (ok) {
-            *reinterpret_cast<uint2 *>(codes + pix * p.ldq + cv * 8) = act8::encode8(v, byte);
-            if ((cv & 3) == 0) scales[pix * p.nb + (cv >> 2)] = (uint8_t)byte;
+    const bool has = pr < p.rows && cv < p.LV, pad = !PACK && pr < p.rows && cv < p.ld / 8;
+    const uint4 keep = act8::keep_bits(cv * 8, p.C), zero = make_uint4(0u, 0u, 0u, 0u);
+    const int step = U * p.rows;
+    uint32_t ox[U], oq[U], os[U];                                // (a thread block's pixels at a time: far below 4 GB)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t r = (uint32_t)(pr + u * p.rows);
+        ox[u] = r * (uint32_t)p.ld * 2u + (uint32_t)cv * 16u;
+        oq[u] = r * (uint32_t)p.ldq + (uint32_t)cv * 8u;
+        os[u] = r * (uint32_t)p.nb + (uint32_t)(cv >> 2);
+    }
+    sm100::grid_dependency_wait();
+    sm100::grid_launch_dependents();
+    for (long long p0 = (long long)blockIdx.x * step; p0 < p.npix; p0 += (long long)gridDim.x * step) {
+        uint8_t *gx = x + p0 * p.ld * 2, *gq = codes + p0 * p.ldq, *gs = scales + p0 * p.nb;
+        const int left = p.npix - p0 < step ? (int)(p.npix - p0) : step;
+        if (PACK) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = has && pr + u * p.rows < left ? *reinterpret_cast<const uint4 *>(gx + ox[u]) : zero;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                v[u] = act8::and4(v[u], keep);
+                const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(v[u]), p.w));
+                if (has && pr + u * p.rows < left) {
+                    *reinterpret_cast<uint2 *>(gq + oq[u]) = act8::encode8(v[u], byte);
+                    if ((cv & 3) == 0) gs[os[u]] = (uint8_t)byte;
+                }
+            }
+        } else {
+            uint2 q[U];
+            uint32_t b[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool ok = has && pr + u * p.rows < left;
+                q[u] = ok ? *reinterpret_cast<const uint2 *>(gq + oq[u]) : make_uint2(0u, 0u);
+                b[u] = ok ? gs[os[u]] : 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float f[8];
+                act8::decode8(q[u], b[u], f);
+                if (pad && pr + u * p.rows < left) *reinterpret_cast<uint4 *>(gx + ox[u]) = act8::and4(act8::pack8(f), keep);
+            }
         }
     }
 }
 
-__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const PackP p, const uint8_t *codes, const uint8_t *scales, uint4 *x)
+template <bool PACK>
+pt_status launch_pack(pt_ctx *c, PackP p, void *x, void *codes, void *scales, cudaStream_t st)
 {
-    const int t = threadIdx.x, out_lv = p.ld / 8;
-    const long long n = p.npix * out_lv;
-    for (long long i = (long long)blockIdx.x * kPackThreads + t; i < n; i += (long long)gridDim.x * kPackThreads) {
-        const long long pix = i / out_lv;
-        const int cv = (int)(i - pix * out_lv);
-        uint4 o = make_uint4(0u, 0u, 0u, 0u);
-        if (cv < p.LV) {
-            float f[8];
-            act8::decode8(*reinterpret_cast<const uint2 *>(codes + pix * p.ldq + cv * 8), scales[pix * p.nb + (cv >> 2)], f);
-            o = act8::and4(act8::pack8(f), act8::keep_bits(cv * 8, p.C));
-        }
-        x[i] = o;
-    }
+    if (p.npix == 0) return PT_OK;
+    p.rl = PACK ? pt_ceil_div(p.LV, p.w) * p.w : p.ld / 8;
+    p.rows = kPackThreads / p.rl;
+    // Blocks of a few rounds each, four to a place on an SM: both passes at 64x56x56x256 take 56.5 us with one round of blocks that share
+    // everything, 53.8 with four, 57.3 with a block for every four pixels a thread. Small tensors: a pixel at a time, spread over more blocks
+    // (128x8x8x41: 3.8 us where four at a time took 4.7).
+    const long long most = (long long)c->sm_count * kPackBlocks * 4, one = (p.npix + p.rows - 1) / p.rows;
+    const bool four = one >= most;
+    const long long need = four ? (one + 3) / 4 : one;
+    PT_CUDA_OK(pt_launch_pdl(four ? pack_kernel<PACK, 4> : pack_kernel<PACK, 1>, dim3((unsigned)(need < most ? need : most)), dim3(kPackThreads), 0, st, p,
+                             (uint8_t *)x, (uint8_t *)codes, (uint8_t *)scales));
+    c->launches += 1;
+    PT_CUDA_OK(cudaGetLastError());
+    return PT_OK;
 }
 
 pt_status pack_params(const pt_ctx *c, const pt_pack_desc *d, const void *x, const void *codes, const void *scales, PackP *p)
@@ -59,8 +101,6 @@ pt_status pack_params(const pt_ctx *c, const pt_pack_desc *d, const void *x, con
     p->npix = d->npix; p->C = d->C; p->ld = d->ld; p->ldq = d->ldq;
     p->LV = (d->C + 7) / 8; p->nb = pt_ceil_div(d->C, act8::kBlock);
     p->w = p->LV >= 3 ? 4 : p->LV;
-    p->rl = pt_ceil_div(p->LV, p->w) * p->w;
-    p->rows = kPackThreads / p->rl;
     return PT_OK;
 }
 
@@ -76,24 +116,12 @@ extern "C" pt_status pt_act_pack(pt_ctx *c, const pt_pack_desc *d, const void *x
 {
     PackP p;
     const pt_status r = pack_params(c, d, x, codes, scales, &p);
-    if (r != PT_OK) return r;
-    if (p.npix == 0) return PT_OK;
-    const long long need = (p.npix + p.rows - 1) / p.rows, most = (long long)c->sm_count * 8;
-    pack_kernel<<<(unsigned)(need < most ? need : most), kPackThreads, 0, (cudaStream_t)stream>>>(p, (const uint4 *)x, (uint8_t *)codes, (uint8_t *)scales);
-    c->launches += 1;
-    PT_CUDA_OK(cudaGetLastError());
-    return PT_OK;
+    return r != PT_OK ? r : launch_pack<true>(c, p, const_cast<void *>(x), codes, scales, (cudaStream_t)stream);
 }
 
 extern "C" pt_status pt_act_unpack(pt_ctx *c, const pt_pack_desc *d, const void *codes, const void *scales, void *x, void *stream)
 {
     PackP p;
     const pt_status r = pack_params(c, d, x, codes, scales, &p);
-    if (r != PT_OK) return r;
-    if (p.npix == 0) return PT_OK;
-    const long long need = (p.npix * (p.ld / 8) + kPackThreads - 1) / kPackThreads, most = (long long)c->sm_count * 8;
-    unpack_kernel<<<(unsigned)(need < most ? need : most), kPackThreads, 0, (cudaStream_t)stream>>>(p, (const uint8_t *)codes, (const uint8_t *)scales, (uint4 *)x);
-    c->launches += 1;
-    PT_CUDA_OK(cudaGetLastError());
-    return PT_OK;
+    return r != PT_OK ? r : launch_pack<false>(c, p, x, const_cast<void *>(codes), const_cast<void *>(scales), (cudaStream_t)stream);
 }
