@@ -23,26 +23,33 @@ constexpr int kGnThreads = 256;              // most consumer threads of a block
 constexpr int kGnTable = 256;                // most groups of a table
 constexpr int kGnMaxLd = 2048;
 constexpr int kGnMaxCluster = 16;
-constexpr int kGnExchange = 512;             // most entries (blocks of the cluster x groups) of one exchange buffer
-constexpr int kGnRows = 2;                   // pixels of a thread's batch
+constexpr int kGnExchange = 1024;            // most entries (blocks of the cluster x groups) of one exchange buffer
+constexpr int kGnSlabs = 32;                 // most slabs of channels
 
 enum { kGnFwd = 0, kGnFwdPack = 1, kGnBwd = 2, kGnBwdPacked = 3 };
 
 __host__ __device__ constexpr bool gn_bwd(int mode) { return mode >= kGnBwd; }
 // Bytes of a thread's place for one pixel: the vectors of x (or codes and the word that holds the scale byte), dy and the residual.
 __host__ __device__ constexpr int gn_slot(int mode, bool res) { return (mode == kGnBwdPacked ? 12 : 16) + (gn_bwd(mode) ? 16 : 0) + (gn_bwd(mode) && res ? 16 : 0); }
+// Pixels of a thread's batch: four in the forward pass (28 us at 64x28x28x371 with a residual, 32 with two); the backward pass, which has
+// twice the constants, is as fast with two.
+__host__ __device__ constexpr int gn_rows(int mode) { return gn_bwd(mode) ? 2 : 4; }
 // Batches of a thread's ring: what two blocks to an SM have room for.
-__host__ __device__ constexpr int gn_batches(int mode, bool res) { return 280 / (kGnRows * gn_slot(mode, res)); }
+__host__ __device__ constexpr int gn_batches(int mode, bool res) { return 290 / (gn_rows(mode) * gn_slot(mode, res)); }
+__host__ __device__ constexpr int gn_ring(int mode, bool res) { return gn_rows(mode) * gn_batches(mode, res) * gn_slot(mode, res); }
 constexpr int kGnBlocks = 2;                 // blocks of an SM: while one exchanges its sums, the other one moves data
+constexpr size_t kGnSmem = 113 * 1024, kGnSmemMost = 226 * 1024;     // shared memory of a block: two on an SM, one
 
 struct GnP {
     int N, HW, C, ld, LV, ldq, nb, G;
+    int slabs, gs;               // slabs of channels, most groups of one; a unit of work is an image's slab
     int w, rl, ppb, threads;     // lanes of a checkpoint's block, lanes of a pixel, pixels the threads cover at a time, threads
     int gl, gc;                  // lanes that add up a group, and those of them that take different channels
     int cl, clusters, share;     // blocks of a cluster, clusters, pixels of a block
     int table;
     unsigned sm_gid, sm_gam, sm_bet, sm_grp, sm_red, sm_xch, sm_acc, sm_ring;
     float eps;
+    uint16_t slab_v[kGnSlabs + 1], slab_g[kGnSlabs + 1];         // first vector and first group of each slab
     uint16_t begin[kGnTable + 1];
 };
 
@@ -53,7 +60,7 @@ struct GnArgs {
     float *save_mean, *save_rstd;
     uint4 *y, *dx, *dres;
     uint8_t *codes, *scales;
-    double *rows;                // backward: [clusters][2][ld] sums of dz and dz * xhat over a cluster's images
+    float *rows;                 // backward: [blocks][2][ld] sums of dz and dz * xhat over a block's units
     float *dgamma, *dbeta;
 };
 
@@ -104,17 +111,14 @@ __device__ __forceinline__ f2 activate2(f2 z)
     return mk2(a > 0.f ? a : (a != a ? a : 0.f), b > 0.f ? b : (b != b ? b : 0.f));
 }
 
-// Two fp64 values into the shared memory of another block of the cluster, visible there behind the cluster's barrier.
-__device__ __forceinline__ void st_cluster_2d(uint32_t addr, double a, double b)
+// Two values into the shared memory of another block of the cluster, visible there behind the cluster's barrier.
+__device__ __forceinline__ void st_cluster_2f(uint32_t addr, float a, float b)
 {
-    asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(addr), "d"(a), "d"(b) : "memory");
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(a), "f"(b) : "memory");
 }
-__device__ __forceinline__ double ld_cluster_d(uint32_t addr)
-{
-    double v;
-    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
-    return v;
-}
+// The two halves of sm100::cluster_barrier. (Shared memory of another block may be written once that block has started.)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // Asynchronous copies of a thread, in groups; waiting for all but the last `PENDING` groups.
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void copy8(uint32_t dst, const void *src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory"); }
@@ -124,11 +128,26 @@ template <int PENDING>
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
 // The largest bf16 <= v (its bits): x > v exactly where x > that, for every bf16 x.
-__device__ __forceinline__ uint32_t bf16_floor(double v)
+__device__ __forceinline__ uint32_t bf16_floor(float v)
 {
-    const uint32_t u = __float_as_uint(__double2float_rd(v));
+    const uint32_t u = __float_as_uint(v);
     if ((u & 0x7fffffffu) > 0x7f800000u) return 0x7fc0u;                 // NaN: no x is above it
     return (u >> 31) ? ((u + 0xffffu) >> 16) : (u >> 16);                // (towards -inf: a negative one's magnitude rounds up)
+}
+
+// ReLU without a residual: z = s*(x - mean) + beta > 0, s = gamma*rstd, for bf16 x, as sg ^ x > th. For s > 0 that is x > mean - beta/s, for
+// s < 0 -x > -(mean - beta/s), for s = 0 a constant. What fp32 leaves uncertain of the limit hardly ever lies about a bf16 value, and then
+// 64 bits decide.
+__device__ __forceinline__ void relu_limit(float mean, float rstd, float gamma, float beta, uint32_t &th, uint32_t &sg)
+{
+    const float s = gamma * rstd, q = beta / s, lim = s < 0.f ? q - mean : mean - q, off = 5e-7f * (fabsf(mean) + fabsf(q));
+    sg = s < 0.f ? 0x8000u : 0u;
+    th = bf16_floor(lim - off);
+    if (th != bf16_floor(lim + off) || !(fabsf(lim) < 1e30f) || !(fabsf(s) > 1e-30f)) {
+        const double sd = (double)gamma * (double)rstd, ld = (double)mean - (double)beta / sd;
+        sg = sd < 0.0 ? 0x8000u : 0u;
+        th = bf16_floor(__double2float_rd(sd == 0.0 ? (beta > 0.f ? -INFINITY : INFINITY) : sd < 0.0 ? -ld : ld));
+    }
 }
 
 // Which of two neighbouring values (bf16 halves of x) have z = gamma*xhat + beta + residual > 0, in 64 bits. Rarely called: fp32 decides
@@ -175,9 +194,9 @@ template <int MODE, int ACT, bool RES>
 __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_constant__ GnP p, const GnArgs a)
 {
     constexpr bool BWD = gn_bwd(MODE), PACK = MODE == kGnFwdPack, PACKED = MODE == kGnBwdPacked;
-    constexpr int B = gn_batches(MODE, RES), U = kGnRows;
+    constexpr int B = gn_batches(MODE, RES), U = gn_rows(MODE);
     // the ring's parts, [B][U][threads] each: x or codes, dy, residual, scale words
-    constexpr uint32_t kXs = PACKED ? 8 : 16, kRowX = kGnThreads * kXs, kRow = kGnThreads * 16, kRowS = kGnThreads * 4;
+    constexpr uint32_t kXs = PACKED ? 8 : 16, kRowX = kGnThreads * kXs, kRow = kGnThreads * 16, kRowS = kGnThreads * 4, kPlace = U * kRow;
     constexpr uint32_t kDy = B * U * kRowX, kRes = kDy + (BWD ? B * U * kRow : 0), kSc = kRes + (BWD && RES ? B * U * kRow : 0);
     extern __shared__ __align__(128) uint8_t smem[];
     uint16_t *gid = reinterpret_cast<uint16_t *>(smem + p.sm_gid);       // [ld] group of a channel
@@ -185,22 +204,16 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     float *grps = reinterpret_cast<float *>(smem + p.sm_grp);            // [2][2][G] of alternating images: mean and rstd (backward), pivot
     float *out = grps + 4 * p.G;                                         // [2][G] rstd and mean (forward), the group's terms of dx (backward)
     float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][17]
-    double2 *xch = reinterpret_cast<double2 *>(smem + p.sm_xch);         // [2][cl][G]
-    double *acc = reinterpret_cast<double *>(smem + p.sm_acc);           // [2][ld]
+    float2 *xch = reinterpret_cast<float2 *>(smem + p.sm_xch);           // [2][cl][gs]
+    float *acc = reinterpret_cast<float *>(smem + p.sm_acc);             // [2][ld] the block's sums of dz and dz * xhat over its units
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = p.threads >> 5;
     const int rank = (int)(blockIdx.x % p.cl), cluster = (int)(blockIdx.x / p.cl);
     const int first = rank * p.share, mine = p.HW - first < p.share ? (p.HW - first > 0 ? p.HW - first : 0) : p.share;
-    const int step = U * p.ppb, NB = (mine + step - 1) / step;           // pixels and number of the block's batches
-    // Threads without a vector of their own (t >= rl * ppb, or lanes that only fill up a checkpoint's block) do what thread 0 does and store
-    // nothing. Vectors of pad lanes only are read and come out as zeros; their codes, which there are none of, are read as vector 0's.
-    int pr = t / p.rl, cv = t - pr * p.rl;
-    const bool lane_ok = pr < p.ppb && cv < p.LV;
-    if (!lane_ok) pr = cv = 0;
-    const int c0 = cv * 8;
-    const bool has = c0 < p.C;                                           // the vector holds channels, not pad lanes only
-    const uint4 keep = act8::keep_bits(c0, p.C);
+    const int step = U * p.ppb, full = mine / step, NB = full * step < mine ? full + 1 : full;     // pixels of a batch; whole batches, and all
+    const int pr0 = t / p.rl, cv0 = t - pr0 * p.rl, pr = pr0 < p.ppb ? pr0 : 0;
     const uint8_t *mine_x = smem + p.sm_ring + t * kXs, *mine_v = smem + p.sm_ring + t * 16, *mine_s = smem + p.sm_ring + kSc + t * 4;
     const uint32_t to_x = sm100::smem_u32(mine_x), to_v = sm100::smem_u32(mine_v), to_s = sm100::smem_u32(mine_s);
+    if (p.cl > 1) cluster_arrive();                                      // (waited for before the first exchange)
     for (int g = t; g < p.G; g += p.threads)
         for (int c = group_begin(p, g), e = group_begin(p, g + 1); c < e; ++c) gid[c] = (uint16_t)g;
     for (int c = p.C + t; c < p.ld; c += p.threads) gid[c] = (uint16_t)(p.G - 1);
@@ -208,99 +221,126 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     sm100::grid_launch_dependents();
     // Offsets in bytes from an image's first pixel of this block: 32 bits, added to addresses that all threads share.
     const uint32_t row = (uint32_t)p.ld * 2u, step_v = (uint32_t)step * row, step_q = (uint32_t)(step * p.ldq), step_s = (uint32_t)(step * p.nb);
-    uint32_t off[U], off_q[U], off_s[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const uint32_t r = (uint32_t)(pr + u * p.ppb);
-        off[u] = r * row + (uint32_t)cv * 16u;
-        off_q[u] = r * (uint32_t)p.ldq + (has ? (uint32_t)c0 : 0u);
-        off_s[u] = r * (uint32_t)p.nb + (has ? (uint32_t)(cv >> 2) : 0u);
-    }
+    const uint32_t row_u = (uint32_t)p.ppb * row, row_q = (uint32_t)(p.ppb * p.ldq), row_s = (uint32_t)(p.ppb * p.nb);   // from one of a thread's pixels to the next
     const auto bytes = [](const void *q) { return reinterpret_cast<const uint8_t *>(q); };
-    struct Src { const uint8_t *x, *dy, *res, *q, *s; };                 // an image's tensors from the block's first pixel on
-    const auto source = [&](int n) {
+    // A unit's tensors from the block's first pixel and the slab's first channel on, and the thread's vector there. Threads without a vector
+    // of their own (t >= rl * ppb, lanes behind a narrower slab or that fill up a checkpoint's block) read vector 0 and store nothing. Vectors
+    // of pad lanes only are read and come out as zeros; their codes, which there are none of, are read as vector 0's.
+    struct Pos { uint32_t v, q, s; };                                    // offsets of a thread's first pixel of a batch: vectors, codes, scales
+    struct Src {
+        const uint8_t *x, *dy, *res, *q, *s;
+        Pos at;                                                          // of batch 0
+    };
+    const auto moved = [&](const Pos &o, int b) { return Pos{o.v + (uint32_t)b * step_v, o.q + (uint32_t)b * step_q, o.s + (uint32_t)b * step_s}; };
+    const int units = p.N * p.slabs;
+    const auto source = [&](int unit) {
         Src g{};
+        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0;
         const size_t pix = (size_t)n * p.HW + first;
-        if (PACKED) { g.q = a.codes_in + pix * p.ldq; g.s = a.scales_in + pix * p.nb; }
-        else g.x = bytes(a.x) + pix * row;
-        if (BWD) g.dy = bytes(a.dy) + pix * row;
-        if (RES) g.res = bytes(a.res) + pix * row;
+        const int cv = pr0 < p.ppb && cv0 < nv ? cv0 : 0, cq = (v0 + cv) * 8 < p.C ? cv : 0;
+        if (PACKED) {
+            g.q = a.codes_in + pix * p.ldq + v0 * 8; g.s = a.scales_in + pix * p.nb + (v0 >> 2);
+            g.at.q = (uint32_t)(pr * p.ldq) + (uint32_t)cq * 8u; g.at.s = (uint32_t)(pr * p.nb) + ((uint32_t)cq >> 2);
+        } else {
+            g.x = bytes(a.x) + pix * row + v0 * 16;
+        }
+        if (BWD) g.dy = bytes(a.dy) + pix * row + v0 * 16;
+        if (RES) g.res = bytes(a.res) + pix * row + v0 * 16;
+        g.at.v = (uint32_t)pr * row + (uint32_t)cv * 16u;
         return g;
     };
-    // batch b of an image into the ring's place s (a multiple of U)
-    const auto bring = [&](const Src &g, int b, int s) {
-        const uint32_t bv = (uint32_t)b * step_v, bq = (uint32_t)b * step_q, bs = (uint32_t)b * step_s;
+    // A batch into the ring's place s (in bytes of the vectors' part); `all`: the thread has all of its pixels, else those of the last batch.
+    const int tail = mine - full * step - pr;                            // pixel u of the last batch is there if u * ppb < tail
+    const auto bring = [&](const Src &g, const Pos &o, uint32_t s, bool all) {
         const auto one = [&](int u) {
             if (PACKED) {
-                copy8(to_x + (uint32_t)(s + u) * kRowX, g.q + (bq + off_q[u]));
-                copy4(to_s + (uint32_t)(s + u) * kRowS, reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(g.s + (bs + off_s[u])) & ~(uintptr_t)3));
+                copy8(to_x + s / 2 + (uint32_t)u * kRowX, g.q + (o.q + (uint32_t)u * row_q));
+                copy4(to_s + s / 4 + (uint32_t)u * kRowS, reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(g.s + (o.s + (uint32_t)u * row_s)) & ~(uintptr_t)3));
             } else {
-                copy16(to_x + (uint32_t)(s + u) * kRowX, g.x + (bv + off[u]));
+                copy16(to_v + s + (uint32_t)u * kRow, g.x + (o.v + (uint32_t)u * row_u));
             }
-            if (BWD) copy16(to_v + kDy + (uint32_t)(s + u) * kRow, g.dy + (bv + off[u]));
-            if (BWD && RES) copy16(to_v + kRes + (uint32_t)(s + u) * kRow, g.res + (bv + off[u]));
+            if (BWD) copy16(to_v + kDy + s + (uint32_t)u * kRow, g.dy + (o.v + (uint32_t)u * row_u));
+            if (BWD && RES) copy16(to_v + kRes + s + (uint32_t)u * kRow, g.res + (o.v + (uint32_t)u * row_u));
         };
-        if ((b + 1) * step <= mine) {
+        if (all) {
 #pragma unroll
             for (int u = 0; u < U; ++u) one(u);
         } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (b * step + u * p.ppb + pr < mine) one(u);
+#pragma unroll 1
+            for (int u = 0; u * p.ppb < tail && u < U; ++u) one(u);
         }
     };
     // (these loads first: behind the ring's copies they would wait for those)
-    const bool ahead = BWD && p.G <= p.threads;                          // an image's statistics are fetched before they are needed
+    const bool ahead = BWD && p.gs <= p.threads;                         // a unit's statistics are fetched before they are needed
     float next_mean = 0.f, next_rstd = 0.f;
-    if (ahead && t < p.G) {
-        next_mean = a.mean[(size_t)cluster * p.G + t];
-        next_rstd = a.rstd[(size_t)cluster * p.G + t];
-    }
-    for (int c = t; c < p.ld; c += p.threads) {
+    const auto fetch_stats = [&](int unit) {
+        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, g = p.slab_g[sl] + t;
+        if (ahead && g < p.slab_g[sl + 1]) {
+            next_mean = a.mean[(size_t)n * p.G + g];
+            next_rstd = a.rstd[(size_t)n * p.G + g];
+        }
+    };
+    fetch_stats(cluster);
+    // (A pad lane's z must not be near 0, see gradient: its beta is 1.) Every load comes before the ring's copies, behind which it would wait
+    // for them all (10 us where the device has started everywhere at once); the first is stored behind them, its latency is theirs.
+    const float gam0 = t < p.C ? a.gamma[t] : 0.f, bet0 = t < p.C ? a.beta[t] : 1.f;
+    for (int c = p.threads + t; c < p.ld; c += p.threads) {
         gam[c] = c < p.C ? a.gamma[c] : 0.f;
-        bet[c] = c < p.C ? a.beta[c] : 1.f;                              // (a pad lane's z must not be near 0, see gradient)
-        if (BWD) acc[c] = acc[p.ld + c] = 0.0;
+        bet[c] = c < p.C ? a.beta[c] : 1.f;
     }
     Src src = source(cluster);
+    __syncthreads();                                                     // (every warp's loads are on their way)
+    // (as much as keeps the memory busy until the first unit's constants are there; more would hold its threads up at the first barrier, copies being
+    // accepted at the rate at which the memory serves them)
+    constexpr int kFirst = 128 / (U * gn_slot(MODE, RES)) < 1 ? 1 : 128 / (U * gn_slot(MODE, RES)) < B ? 128 / (U * gn_slot(MODE, RES)) : B;
 #pragma unroll 1
-    for (int b = 0; b < B; ++b) {
-        if (b < NB) bring(src, b, b * U);
+    for (int b = 0; b < kFirst; ++b) {
+        if (b < NB) bring(src, moved(src.at, b), (uint32_t)b * kPlace, b < full);
         copy_commit();
     }
+    if (t < p.ld) { gam[t] = gam0; bet[t] = bet0; }
+    if (BWD)
+        for (int c = t; c < 2 * p.ld; c += p.threads) acc[c] = 0.f;
     int dir = 0, it = 0;
-    const double inv_hw = 1.0 / (double)p.HW;
+    const float inv_hw = 1.f / (float)p.HW;
     const int whole = p.HW / p.share;                                    // blocks with all their pixels
-    const double rest = (double)(p.HW - whole * p.share);                // pixels of the one behind them
-    for (int n = cluster; n < p.N; n += p.clusters, dir ^= 1, ++it) {
+    const float rest = (float)(p.HW - whole * p.share);                  // pixels of the one behind them
+    for (int unit = cluster; unit < units; unit += p.clusters, dir ^= 1, ++it) {
+        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0, gb = p.slab_g[sl], ge = p.slab_g[sl + 1];
+        const bool lane_ok = pr0 < p.ppb && cv0 < nv;
+        const int cv = v0 + (lane_ok ? cv0 : 0), c0 = cv * 8;           // the thread's vector and its first channel
+        const bool has = c0 < p.C;                                       // it holds channels, not pad lanes only
+        const uint4 keep = act8::keep_bits(c0, p.C);
         const size_t base = (size_t)n * p.HW + first;                    // the block's first pixel
-        const Src next = source(n + p.clusters < p.N ? n + p.clusters : n);
+        const bool more = unit + p.clusters < units;
         // (so that a batch of the first walk always has B - 1 groups behind it when it is waited for)
         if (it > 0)
             for (int b = NB; b < B; ++b) copy_commit();
         // ---- what the first walk needs of every group: the statistics (backward), or a value near its mean (forward)
         float *grp = grps + (it & 1) * 2 * p.G;
         if (BWD && ahead) {
-            if (t < p.G) { grp[t] = next_mean; grp[p.G + t] = next_rstd; }
+            if (gb + t < ge) { grp[gb + t] = next_mean; grp[p.G + gb + t] = next_rstd; }
         } else if (BWD) {
-            for (int g = t; g < p.G; g += p.threads) {
+            for (int g = gb + t; g < ge; g += p.threads) {
                 grp[g] = a.mean[(size_t)n * p.G + g];
                 grp[p.G + g] = a.rstd[(size_t)n * p.G + g];
             }
         } else {
-            copy_wait<B - 1>();
+            if (it == 0) copy_wait<kFirst - 1>();
+            else copy_wait<B - 1>();
             __syncthreads();
             // the average over the group's channels of the block's first pixels: as near the mean as a few values tell
             const int rows = min(min(4, p.ppb), mine), per = 32 / p.gl, l = lane & (p.gl - 1);
             const uint8_t *px = smem + p.sm_ring + (dir ? (B - 1) * U * kRowX : 0u);
-            for (int g0 = warp * per; g0 < p.G; g0 += warps * per) {
+            for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
                 const int g = g0 + lane / p.gl;
-                const int b = g < p.G ? group_begin(p, g) : 0, e = g < p.G ? group_begin(p, g + 1) : 0;
+                const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
                 float v = 0.f;
                 for (int c = b + l; c < e; c += p.gl)
                     for (int r = 0; r < rows; ++r)
-                        v += __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(px + (size_t)(r * p.rl + (c >> 3)) * 16 + (c & 7) * 2));
+                        v += __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(px + (size_t)(r * p.rl + (c >> 3) - v0) * 16 + (c & 7) * 2));
                 for (int o = p.gl >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (l == 0 && g < p.G) grp[g] = rows > 0 ? v / (float)(rows * (e - b)) : 0.f;
+                if (l == 0 && g < ge) grp[g] = rows > 0 ? v / (float)(rows * (e - b)) : 0.f;
             }
         }
         __syncthreads();
@@ -318,14 +358,12 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 if (BWD) {
                     kk[j] = gam[c] * grp[p.G + g];
                     b[j] = bet[c];
-                    be_max = fmaxf(be_max, 1e-6f * fabsf(b[j]));
+                    be_max = fmaxf(be_max, 1e-6f * fmaxf(fabsf(b[j]), fabsf(fmaf(m[j], kk[j], b[j]))));
                     if (ACT == PT_ACT_SILU) b[j] *= -kLog2e;
                 }
                 if (BWD && ACT == PT_ACT_RELU && !RES) {
-                    // z = s*(x - mean) + beta > 0  <=>  x > mean - beta/s (s > 0), -x > -(mean - beta/s) (s < 0); a constant for s = 0
-                    const double s = (double)gam[c] * (double)grp[p.G + g], bj = (double)bet[c];
-                    const double lim = s == 0.0 ? (bj > 0.0 ? -INFINITY : INFINITY) : (double)grp[g] - bj / s;
-                    const uint32_t th = bf16_floor(s < 0.0 ? -lim : lim), sg = s < 0.0 ? 0x8000u : 0u;
+                    uint32_t th, sg;
+                    relu_limit(grp[g], grp[p.G + g], gam[c], bet[c], th, sg);
                     thr[j >> 1] = j & 1 ? thr[j >> 1] | th << 16 : th;
                     sgn[j >> 1] = j & 1 ? sgn[j >> 1] | sg << 16 : sg;
                 }
@@ -340,18 +378,17 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 }
             }
         }
-        // pixel u of a batch, at the ring's place s; bs: the batch's offset in the scales
-        const uint32_t s_base = PACKED ? (uint32_t)(base * p.nb) : 0u;   // (the buffer starts on a word)
-        const auto fetch = [&](Raw &w, uint32_t bs, int s, int u) {
+        // pixel u of a batch at the ring's place s; os: the thread's place in the scales
+        const uint32_t s_base = PACKED ? (uint32_t)(reinterpret_cast<uintptr_t>(src.s) & 3u) : 0u;
+        const auto fetch = [&](Raw &w, uint32_t os, uint32_t s, int u) {
             if (PACKED) {
-                w.q = *reinterpret_cast<const uint2 *>(mine_x + (uint32_t)(s + u) * kRowX);
-                const uint32_t sc = s_base + bs + off_s[u];
-                w.byte = *reinterpret_cast<const uint32_t *>(mine_s + (uint32_t)(s + u) * kRowS) >> ((sc & 3u) * 8u) & 0xffu;
+                w.q = *reinterpret_cast<const uint2 *>(mine_x + s / 2 + (uint32_t)u * kRowX);
+                w.byte = *reinterpret_cast<const uint32_t *>(mine_s + s / 4 + (uint32_t)u * kRowS) >> (((s_base + os + (uint32_t)u * row_s) & 3u) * 8u) & 0xffu;
             } else {
-                w.x = *reinterpret_cast<const uint4 *>(mine_x + (uint32_t)(s + u) * kRowX);
+                w.x = *reinterpret_cast<const uint4 *>(mine_v + s + (uint32_t)u * kRow);
             }
-            if (BWD) w.dy = *reinterpret_cast<const uint4 *>(mine_v + kDy + (uint32_t)(s + u) * kRow);
-            if (BWD && RES) w.res = *reinterpret_cast<const uint4 *>(mine_v + kRes + (uint32_t)(s + u) * kRow);
+            if (BWD) w.dy = *reinterpret_cast<const uint4 *>(mine_v + kDy + s + (uint32_t)u * kRow);
+            if (BWD && RES) w.res = *reinterpret_cast<const uint4 *>(mine_v + kRes + s + (uint32_t)u * kRow);
         };
         const auto values = [&](Raw &w, f2 (&x)[4]) {                   // x as fp32 pairs (and, from codes, as bf16 words)
             if (PACKED) {
@@ -361,7 +398,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 x[0] = from_bf(w.x.x); x[1] = from_bf(w.x.y); x[2] = from_bf(w.x.z); x[3] = from_bf(w.x.w);
             }
         };
-        // dz: in place of dy's words where it is dy's bits under a mask, and as pairs. d = x - mean.
+        // dz: in place of dy's words where it is dy's bits under a mask, and as pairs. d: what k and be are about, x - mean in the first
+        // walk, x in the second.
         const auto gradient = [&](Raw &w, const f2 (&d)[4], f2 (&z)[4], f2 (&dz)[4], bool want_z) {
             uint32_t *g = reinterpret_cast<uint32_t *>(&w.dy);
             const uint32_t *xb = reinterpret_cast<const uint32_t *>(&w.x), *rb = reinterpret_cast<const uint32_t *>(&w.res);
@@ -379,7 +417,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 }
             }
             if (ACT == PT_ACT_RELU && RES) {
-                // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |beta| + |residual|: there 64 bits decide. One test for the
+                // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |residual| + |beta| + |beta - mean*k| (the
+                // second walk's constant): there 64 bits decide. One test for the
                 // eight values, the least |z| against the largest |residual|: it is passed a few times in a hundred thousand.
                 float zz[8], low = INFINITY;
                 uint32_t top = 0u;
@@ -394,11 +433,10 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // (gamma = 0, a pruned channel's or a pad lane's: z = beta + residual, of the right sign in fp32)
-                        float k0, k1, b0, b1;
+                        float k0, k1;
                         un2(k[i], k0, k1);
-                        un2(be[i], b0, b1);
-                        const bool near0 = k0 != 0.f && fabsf(zz[2 * i]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] << 16)) + fabsf(b0));
-                        const bool near1 = k1 != 0.f && fabsf(zz[2 * i + 1]) <= 1e-6f * (fabsf(__uint_as_float(rb[i] & 0xffff0000u)) + fabsf(b1));
+                        const bool near0 = k0 != 0.f && fabsf(zz[2 * i]) <= fmaf(fabsf(__uint_as_float(rb[i] << 16)), 1e-6f, be_max);
+                        const bool near1 = k1 != 0.f && fabsf(zz[2 * i + 1]) <= fmaf(fabsf(__uint_as_float(rb[i] & 0xffff0000u)), 1e-6f, be_max);
                         uint32_t m = (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
                         if (near0 || near1) m = exact_mask(xb[i], rb[i], c0 + 2 * i, gid, grp, p.G, gam, bet);
                         g[i] &= m;
@@ -421,6 +459,12 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             }
         };
 
+        if (it == 0)
+#pragma unroll 1
+            for (int b = kFirst; b < B; ++b) {
+                if (b < NB) bring(src, moved(src.at, b), (uint32_t)b * kPlace, b < full);
+                copy_commit();
+            }
         // ---- first walk: sums of x - pivot and its square, or of dz and dz * (x - mean)
         f2 s0[4], s1[4];
 #pragma unroll
@@ -456,64 +500,65 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             flushed = true;
         };
         // the ring's places in the order of the walk, and where they begin and end
-        const int s_first = dir ? (B - 1) * U : 0, s_last = dir ? 0 : (B - 1) * U, s_step = dir ? -U : U;
-        int s = s_first;
+        const uint32_t s_first = dir ? (B - 1) * kPlace : 0u, s_last = dir ? 0u : (B - 1) * kPlace, s_step = dir ? 0u - kPlace : kPlace;
+        uint32_t s = s_first;
+        Pos here = src.at, then = moved(src.at, B);
         for (int b = 0; b < NB; ++b) {
             copy_wait<B - 1>();
-            const int left = mine - b * step - pr;                       // pixel u is there if u * ppb < left
-            const uint32_t bs = (uint32_t)b * step_s;
+            const bool all = b < full;
             if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
-                uint8_t *gq = a.codes + base * p.ldq, *gs = a.scales + base * p.nb;
-                const uint32_t bq = (uint32_t)b * step_q;
+                uint8_t *gq = a.codes + base * p.ldq + (size_t)b * step_q, *gs = a.scales + base * p.nb + (size_t)b * step_s;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const bool ok = u * p.ppb < left;
+                    const bool ok = all || u * p.ppb < tail;
                     Raw w;
                     w.x = make_uint4(0u, 0u, 0u, 0u);
                     if (ok) {
-                        fetch(w, bs, s, u);
+                        fetch(w, here.s, s, u);
                         count(w);
                     }
                     w.x = act8::and4(w.x, keep);
                     if (!lane_ok) w.x = make_uint4(0u, 0u, 0u, 0u);
                     const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(w.x), p.w));
                     if (ok && lane_ok && has) {
-                        *reinterpret_cast<uint2 *>(gq + (bq + off_q[u])) = act8::encode8(w.x, byte);
-                        if ((cv & 3) == 0) gs[bs + off_s[u]] = (uint8_t)byte;
+                        *reinterpret_cast<uint2 *>(gq + (uint32_t)(pr * p.ldq + c0 + u * (int)row_q)) = act8::encode8(w.x, byte);
+                        if ((cv & 3) == 0) gs[(uint32_t)(pr * p.nb + (cv >> 2) + u * (int)row_s)] = (uint8_t)byte;
                     }
                 }
-            } else if ((b + 1) * step <= mine) {                         // two pixels at a time, their loads first
+            } else if (all) {                                            // a batch at a time, its loads first
                 Raw w[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) fetch(w[u], bs, s, u);
+                for (int u = 0; u < U; ++u) fetch(w[u], here.s, s, u);
 #pragma unroll
                 for (int u = 0; u < U; ++u) count(w[u]);
-            } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u * p.ppb < left) {
-                        Raw w;
-                        fetch(w, bs, s, u);
-                        count(w);
-                    }
+            } else {                                                     // (one copy of the code: a small image is one such batch)
+#pragma unroll 1
+                for (int u = 0; u * p.ppb < tail && u < U; ++u) {
+                    Raw w;
+                    fetch(w, here.s, s, u);
+                    count(w);
+                }
             }
-            if (b + B < NB) bring(src, b + B, s);                        // (the last B batches stay for the second walk)
+            if (b + B < NB) bring(src, then, s, b + B < full);           // (the last B batches stay for the second walk)
             copy_commit();
-            if ((b & 31) == 31 || b == NB - 1) flush();
+            then = moved(then, 1);
+            here = moved(here, 1);
+            if ((b & (64 / U - 1)) == 64 / U - 1 || b == NB - 1) flush();
             s = s == s_last ? s_first : s + s_step;
         }
         if (NB == 0) flush();
         // ---- a group's sums over the threads' rows and its channels
         __syncthreads();
+        if (p.cl > 1 && it == 0) cluster_wait();
         {
             // a group's lanes: gc of them take its channels, the others more of the threads' rows
             const int per = 32 / p.gl, l = lane & (p.gl - 1), lc = l & (p.gc - 1), lr = l / p.gc, nr = p.gl / p.gc, buf = it & 1;
-            for (int g0 = warp * per; g0 < p.G; g0 += warps * per) {
+            for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
                 const int g = g0 + lane / p.gl;
-                const int b = g < p.G ? group_begin(p, g) : 0, e = g < p.G ? group_begin(p, g + 1) : 0;
+                const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
                 float f0 = 0.f, f1 = 0.f;
                 for (int c = b + lc; c < e; c += p.gc) {
-                    const float *src = red + (lr * p.rl + (c >> 3)) * 17 + (c & 7);
+                    const float *src = red + (lr * p.rl + (c >> 3) - v0) * 17 + (c & 7);
                     float w0 = 0.f, w1 = 0.f;
 #pragma unroll 4
                     for (int r = lr; r < p.ppb; r += nr, src += nr * p.rl * 17) { w0 += src[0]; w1 += src[8]; }
@@ -525,49 +570,46 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     f0 += __shfl_xor_sync(0xffffffffu, f0, o);
                     f1 += __shfl_xor_sync(0xffffffffu, f1, o);
                 }
-                double v0 = (double)f0, v1 = (double)f1;
                 if (!BWD) {                                              // the block's mean and sum of squares about it
-                    const double cnt = (double)mine * (double)(e - b), d = cnt > 0.0 ? v0 / cnt : 0.0;
-                    v1 = v1 - v0 * d;
-                    v0 = g < p.G && mine > 0 ? (double)grp[g] + d : 0.0;
-                    if (v1 < 0.0) v1 = 0.0;
+                    const float d = mine > 0 ? f0 / ((float)mine * (float)(e - b)) : 0.f;
+                    f1 = fmaxf(f1 - f0 * d, 0.f);
+                    f0 = g < ge && mine > 0 ? grp[g] + d : 0.f;
                 }
-                if (g < p.G)
+                if (g < ge)
                     for (int r = l; r < p.cl; r += p.gl) {
-                        double2 *to = xch + ((size_t)buf * p.cl + rank) * p.G + g;
-                        if (p.cl == 1) *to = make_double2(v0, v1);
-                        else st_cluster_2d(sm100::map_to_rank(sm100::smem_u32(to), (uint32_t)r), v0, v1);
+                        float2 *to = xch + (buf * p.cl + rank) * p.gs + (g - gb);
+                        if (p.cl == 1) *to = make_float2(f0, f1);
+                        else st_cluster_2f(sm100::map_to_rank(sm100::smem_u32(to), (uint32_t)r), f0, f1);
                     }
             }
+            // (divided before the wait)
+            const int own_g = gb + t;
+            const float im0 = own_g < ge ? inv_hw / (float)(group_begin(p, own_g + 1) - group_begin(p, own_g)) : 0.f;
             if (p.cl > 1) sm100::cluster_barrier();
             else __syncthreads();
             // ---- the image's values from those of the cluster's blocks, in order
-            for (int g = t; g < p.G; g += p.threads) {
-                const double2 *v = xch + (size_t)buf * p.cl * p.G + g;
+            for (int g = own_g; g < ge; g += p.threads) {
+                const float2 *v = xch + buf * p.cl * p.gs + (g - gb);
                 const int size = group_begin(p, g + 1) - group_begin(p, g);
-                const double m = (double)p.HW * (double)size;
-                double v0 = 0.0, v1 = 0.0;
+                const float im = g == own_g ? im0 : inv_hw / (float)size;
                 if (BWD) {
-                    for (int r = 0; r < p.cl; ++r) { v0 += v[(size_t)r * p.G].x; v1 += v[(size_t)r * p.G].y; }
-                    const double rs = (double)grp[p.G + g], im = 1.0 / m;
-                    const double t1 = -(rs * rs * rs * v1 * im);
-                    out[g] = (float)(-(rs * v0 * im) - t1 * (double)grp[g]);
-                    out[p.G + g] = (float)t1;
+                    float e0 = 0.f, e1 = 0.f;
+                    for (int r = 0; r < p.cl; ++r) { e0 += v[r * p.gs].x; e1 += v[r * p.gs].y; }
+                    const float rs = grp[p.G + g], t1 = -(rs * rs * rs * e1 * im);
+                    out[g] = fmaf(-t1, grp[g], -(rs * e0 * im));
+                    out[p.G + g] = t1;
                 } else {
-                    // all blocks but the last have `share` pixels (those behind the last have none, and sent zeros)
-                    for (int r = 0; r < whole; ++r) v0 += v[(size_t)r * p.G].x;
-                    const double last = rest > 0.0 ? v[(size_t)whole * p.G].x : 0.0;
-                    v0 = (v0 * (double)p.share + last * rest) * inv_hw;
-                    double spread = 0.0;
-                    for (int r = 0; r < whole; ++r) {
-                        const double d = v[(size_t)r * p.G].x - v0;
-                        spread += d * d;
-                        v1 += v[(size_t)r * p.G].y;
-                    }
-                    spread = spread * (double)p.share + (last - v0) * (last - v0) * rest;
-                    if (rest > 0.0) v1 += v[(size_t)whole * p.G].y;
-                    v1 += spread * (double)size;
-                    const float fm = (float)v0, fr = (float)rsqrt(v1 / m + (double)p.eps);
+                    // All blocks but the last have `share` pixels (those behind the last have none). Means are averaged as differences from the
+                    // first block's, and the squares of what the blocks' means differ by belong to the variance.
+                    const float ref = v[0].x, last = rest > 0.f ? v[whole * p.gs].x - ref : 0.f;
+                    float d = 0.f, sq = 0.f;
+                    for (int r = 0; r < whole; ++r) { d += v[r * p.gs].x - ref; sq += v[r * p.gs].y; }
+                    if (rest > 0.f) sq += v[whole * p.gs].y;
+                    d = (d * (float)p.share + last * rest) * inv_hw;
+                    float spread = 0.f;
+                    for (int r = 0; r < whole; ++r) { const float o = v[r * p.gs].x - ref - d; spread = fmaf(o, o, spread); }
+                    spread = spread * (float)p.share + (last - d) * (last - d) * rest;
+                    const float fm = ref + d, fr = 1.f / sqrtf(fmaf(fmaf(spread, (float)size, sq), im, p.eps));
                     out[g] = fr;
                     out[p.G + g] = fm;
                     if (rank == 0) {
@@ -600,17 +642,16 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             for (int i = 0; i < 4; ++i) {
                 c1[i] = mk2(u[2 * i], u[2 * i + 1]);
                 c2[i] = mk2(v[2 * i], v[2 * i + 1]);
-                if (BWD && !(ACT == PT_ACT_RELU && RES)) be[i] = fma2(nm[i], kz[i], be[i]);
+                if (BWD) be[i] = fma2(nm[i], kz[i], be[i]);
             }
         }
-        if (ahead && t < p.G && n + p.clusters < p.N) {
-            next_mean = a.mean[(size_t)(n + p.clusters) * p.G + t];
-            next_rstd = a.rstd[(size_t)(n + p.clusters) * p.G + t];
-        }
+        if (more) fetch_stats(unit + p.clusters);
         // ---- second walk, backwards: the results
         const bool want_y = !BWD || (PACKED && a.y);
-        // gx, gr, gy: the batch's first pixel in dx, dresidual and y
-        const auto result = [&](Raw &w, uint8_t *gx, uint8_t *gr, uint8_t *gy, uint32_t at) {
+        // the unit's first pixel in dx, dresidual and y
+        const size_t unit_v = base * row + (size_t)v0 * 16;
+        uint8_t *const gx = reinterpret_cast<uint8_t *>(a.dx) + unit_v, *const gr = reinterpret_cast<uint8_t *>(a.dres) + unit_v, *const gy = reinterpret_cast<uint8_t *>(a.y) + unit_v;
+        const auto result = [&](Raw &w, uint32_t at) {
             f2 x[4], z[4], dz[4];
             uint4 o;
             uint32_t *ow = reinterpret_cast<uint32_t *>(&o);
@@ -625,10 +666,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 }
                 if (lane_ok) *reinterpret_cast<uint4 *>(gy + at) = act8::and4(o, keep);
             } else {
-                f2 d[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) d[i] = ACT == PT_ACT_RELU && RES ? add2(x[i], nm[i]) : x[i];
-                gradient(w, d, z, dz, want_y);
+                gradient(w, x, z, dz, want_y);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ow[i] = to_bf(fma2(k[i], dz[i], fma2(x[i], c2[i], c1[i])));
                 if (lane_ok) *reinterpret_cast<uint4 *>(gx + at) = act8::and4(o, keep);
@@ -644,97 +682,100 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             }
         };
         Raw ahead_w[U];                                                  // forward: the residual, a batch ahead
-        const auto residual = [&](int b) {
-            if (!BWD && RES && b >= 0) {
+        here = moved(src.at, NB - 1);
+        const uint8_t *const res_v = RES ? src.res : nullptr;
+        const auto residual = [&](uint32_t at, bool all) {
+            if (!BWD && RES)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (b * step + u * p.ppb + pr < mine) ahead_w[u].res = *reinterpret_cast<const uint4 *>(src.res + ((uint32_t)b * step_v + off[u]));
-            }
+                    if (all || u * p.ppb < tail) ahead_w[u].res = *reinterpret_cast<const uint4 *>(res_v + (at + (uint32_t)u * row_u));
         };
-        residual(NB - 1);
+        if (NB > 0) residual(here.v, NB == full);
         const int kept = NB < B ? NB : B;
-        uint8_t *gx = reinterpret_cast<uint8_t *>(a.dx) + base * row, *gr = reinterpret_cast<uint8_t *>(a.dres) + base * row, *gy = reinterpret_cast<uint8_t *>(a.y) + base * row;
         for (int b = NB - 1; b >= 0; --b) {
             s = s == s_first ? s_last : s - s_step;
             copy_wait<B - 1>();
-            const int left = mine - b * step - pr;
-            const uint32_t bv = (uint32_t)b * step_v, bs = (uint32_t)b * step_s;
             Raw w[U];
             if (!BWD && RES) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) w[u].res = ahead_w[u].res;
-                residual(b - 1);
+                if (b > 0) residual(here.v - step_v, true);
             }
-            if ((b + 1) * step <= mine) {
+            if (b < full) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) fetch(w[u], bs, s, u);
+                for (int u = 0; u < U; ++u) fetch(w[u], here.s, s, u);
 #pragma unroll
-                for (int u = 0; u < U; ++u) result(w[u], gx, gr, gy, bv + off[u]);
+                for (int u = 0; u < U; ++u) result(w[u], here.v + (uint32_t)u * row_u);
             } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u * p.ppb < left) {
-                        fetch(w[u], bs, s, u);
-                        result(w[u], gx, gr, gy, bv + off[u]);
-                    }
+#pragma unroll 1
+                for (int u = 0; u * p.ppb < tail && u < U; ++u) {
+                    Raw v;
+                    if (!BWD && RES) v.res = *reinterpret_cast<const uint4 *>(res_v + (here.v + (uint32_t)u * row_u));
+                    fetch(v, here.s, s, u);
+                    result(v, here.v + (uint32_t)u * row_u);
+                }
             }
-            // the place takes an earlier batch, or one of the cluster's next image: its first goes to the place that is free first
-            if (b >= B) bring(src, b - B, s);
-            else if (n + p.clusters < p.N) bring(next, kept - 1 - b, dir ? (kept - 1 - b) * U : (B - kept + b) * U);
+            // the place takes an earlier batch, or one of the cluster's next unit: its first goes to the place that is free first
+            if (b >= B) {
+                bring(src, moved(here, -B), s, true);
+            } else if (more) {
+                const int m = kept - 1 - b;
+                if (m == 0) src = source(unit + p.clusters);
+                bring(src, moved(src.at, m), (uint32_t)(dir ? m : B - 1 - m) * kPlace, m < full);
+            }
             copy_commit();
+            here = moved(here, -1);
         }
-        src = next;
         if (BWD)                                                         // the images' sums of dz and dz * xhat, a channel's
-            for (int c = t; c < p.C; c += p.threads) {
-                const float *src = red + (c >> 3) * 17 + (c & 7);
-                float v0 = 0.f, v1 = 0.f, u0 = 0.f, u1 = 0.f;
+            for (int c = v0 * 8 + t; c < min(p.C, (v0 + nv) * 8); c += p.threads) {
+                const float *src = red + ((c >> 3) - v0) * 17 + (c & 7);
+                float w0 = 0.f, w1 = 0.f, u0 = 0.f, u1 = 0.f;
                 int r = 0;
                 for (; r + 1 < p.ppb; r += 2, src += 2 * p.rl * 17) {
-                    v0 += src[0]; v1 += src[8];
+                    w0 += src[0]; w1 += src[8];
                     u0 += src[p.rl * 17]; u1 += src[p.rl * 17 + 8];
                 }
-                if (r < p.ppb) { v0 += src[0]; v1 += src[8]; }
-                acc[c] += (double)v0 + (double)u0;
-                acc[p.ld + c] += ((double)v1 + (double)u1) * (double)grp[p.G + gid[c]];
+                if (r < p.ppb) { w0 += src[0]; w1 += src[8]; }
+                acc[c] += w0 + u0;
+                acc[p.ld + c] += (w1 + u1) * grp[p.G + gid[c]];
             }
     }
-    // ---- the cluster's sums over its images
+    // ---- the block's row of sums
     if (BWD) {
-        if (p.cl > 1) sm100::cluster_barrier();
-        else __syncthreads();
-        const int per = (2 * p.ld + p.cl - 1) / p.cl;
-        for (int e = rank * per + t; e < min(2 * p.ld, (rank + 1) * per); e += p.threads) {
-            double v = 0.0;
-            if (p.cl == 1) v = acc[e];
-            else
-                for (int r = 0; r < p.cl; ++r) v += ld_cluster_d(sm100::map_to_rank(sm100::smem_u32(acc + e), (uint32_t)r));
+        __syncthreads();
+        for (int e = t; e < 2 * p.ld; e += p.threads) {
             const int s = e >= p.ld, c = e - s * p.ld;
-            if (p.clusters > 1) a.rows[(size_t)cluster * 2 * p.ld + e] = v;
-            else if (c < p.C) (s ? a.dgamma : a.dbeta)[c] = (float)v;
+            if (gridDim.x > 1) a.rows[(size_t)blockIdx.x * 2 * p.ld + e] = acc[e];
+            else if (c < p.C) (s ? a.dgamma : a.dbeta)[c] = acc[e];
         }
     }
-    if (p.cl > 1) sm100::cluster_barrier();
 }
 
-// dgamma, dbeta: the clusters' rows. A block owns 32 columns; its warps take every 32nd row each, then one thread per column adds the
-// warps' sums: a fixed order, fp64.
-__global__ void __launch_bounds__(1024) gn_finish_kernel(const double *rows, int n, int C, int ld, float *dgamma, float *dbeta)
+// dgamma, dbeta: the blocks' rows. A block owns 32 columns; a warp adds every 32nd row of them, all loads before the first addition, then
+// a column's 32 sums: a fixed order, chains of at most ten.
+__global__ void __launch_bounds__(1024) gn_finish_kernel(const float *rows, int n, int C, int ld, float *dgamma, float *dbeta)
 {
-    __shared__ double part[32][33];
+    __shared__ float part[32][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, e = blockIdx.x * 32 + lane;
     sm100::grid_dependency_wait();
     sm100::grid_launch_dependents();
-    double v = 0.0;
-    if (e < 2 * ld)
-        for (int r = warp; r < n; r += 32) v += rows[(size_t)r * 2 * ld + e];
+    const float *src = rows + e;
+    const size_t pitch = (size_t)2 * ld;
+    float v = 0.f;
+    for (int r0 = warp; r0 < n; r0 += 10 * 32) {                         // (296 rows are one round)
+        float x[10];
+#pragma unroll
+        for (int i = 0; i < 10; ++i) x[i] = e < 2 * ld && r0 + 32 * i < n ? __ldg(src + (r0 + 32 * i) * pitch) : 0.f;
+#pragma unroll
+        for (int i = 0; i < 10; ++i) v += x[i];
+    }
     part[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && e < 2 * ld) {
-        v = 0.0;
-        for (int k = 0; k < 32; ++k) v += part[k][lane];
-        const int s = e >= ld, c = e - s * ld;
-        if (c < C) (s ? dgamma : dbeta)[c] = (float)v;
-    }
+    v = part[lane][warp];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    const int f = blockIdx.x * 32 + warp, s = f >= ld, c = f - s * ld;
+    if (lane == 0 && f < 2 * ld && c < C) (s ? dgamma : dbeta)[c] = v;
 }
 
 typedef void (*GnKernel)(GnP, GnArgs);
@@ -787,95 +828,196 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     return PT_OK;
 }
 
-// The launch shape for clusters of cl blocks: how the threads cover a pixel row, and the shared memory's parts. Returns its bytes.
+int gn_begin(const GnP &p, int g) { return p.table ? p.begin[g] : g * (p.C / p.G); }
+
+// Cuts the channels into about `want` slabs of whole groups and whole vectors (whole blocks of 32 channels where there is a checkpoint).
+void gn_slabs(GnP *p, int want, bool blocks)
+{
+    const int align = blocks ? act8::kBlock : 8;
+    p->slabs = 1;
+    p->gs = 0;
+    int last = 0;
+    const auto cut = [&](int v, int g) {
+        p->slab_v[p->slabs] = (uint16_t)v; p->slab_g[p->slabs] = (uint16_t)g;
+        p->gs = p->gs > g - last ? p->gs : g - last;
+        last = g;
+    };
+    p->slab_v[0] = p->slab_g[0] = 0;
+    for (int g = 1; g < p->G && p->slabs < want; ++g) {
+        const int c = gn_begin(*p, g);
+        // the first boundary at or behind the place of the next cut
+        if (c % align == 0 && (long long)c * want >= (long long)p->slabs * p->C) { cut(c / 8, g); p->slabs += 1; }
+    }
+    cut(p->LV, p->G);
+    p->rl = 0;
+    for (int s = 0; s < p->slabs; ++s) {
+        const int w = p->slab_v[s + 1] - p->slab_v[s];
+        p->rl = p->rl > w ? p->rl : w;
+    }
+}
+
+// The launch shape for clusters of cl blocks: how the threads cover a slab's pixels, and the shared memory's parts. Returns its bytes.
 size_t gn_shape(GnP *p, int mode, bool res, int cl)
 {
     p->cl = cl;
     p->share = pt_ceil_div(p->HW, cl);
-    p->rl = mode == kGnFwdPack ? pt_ceil_div(p->LV, p->w) * p->w : p->LV;
+    if (mode == kGnFwdPack) p->rl = pt_ceil_div(p->rl, p->w) * p->w;
     p->ppb = kGnThreads / p->rl;
     if (p->ppb > p->share) p->ppb = p->share;
     p->threads = (p->rl * p->ppb + 31) / 32 * 32;
     // lanes of a group: as many as there are for it; as many of them for its channels as it has
-    int most = pt_ceil_div(p->C, p->G);
-    if (p->table)
-        for (int g = 0; g < p->G; ++g) most = most > p->begin[g + 1] - p->begin[g] ? most : p->begin[g + 1] - p->begin[g];
+    int most = 1;
+    for (int g = 0; g < p->G; g += p->table ? 1 : p->G) most = most > gn_begin(*p, g + 1) - gn_begin(*p, g) ? most : gn_begin(*p, g + 1) - gn_begin(*p, g);
     p->gl = 1;
-    while (p->gl < 32 && 2 * p->gl * p->G <= p->threads && p->gl < most * p->ppb) p->gl *= 2;
+    while (p->gl < 32 && 2 * p->gl * p->gs <= p->threads && p->gl < most * p->ppb) p->gl *= 2;
     p->gc = 1;
     while (p->gc < p->gl && p->gc < most) p->gc *= 2;
     size_t at = 0;
     const auto part = [&](unsigned *off, size_t bytes) { *off = (unsigned)at; at += pt_align_up(bytes, 16); };
-    part(&p->sm_ring, (size_t)kGnThreads * kGnRows * gn_batches(mode, res) * gn_slot(mode, res));
+    part(&p->sm_ring, (size_t)kGnThreads * gn_ring(mode, res));
     part(&p->sm_gid, (size_t)p->ld * 2);
     part(&p->sm_gam, (size_t)p->ld * 4);
     part(&p->sm_bet, (size_t)p->ld * 4);
     part(&p->sm_grp, (size_t)p->G * 6 * 4);
     part(&p->sm_red, (size_t)p->threads * 17 * 4);
-    part(&p->sm_xch, (size_t)2 * cl * p->G * 16);
-    part(&p->sm_acc, gn_bwd(mode) ? (size_t)2 * p->ld * 8 : 0);
+    part(&p->sm_xch, (size_t)2 * cl * p->gs * 8);
+    part(&p->sm_acc, gn_bwd(mode) ? (size_t)2 * p->ld * 4 : 0);
     return at;
 }
 
 bool aligned16(const void *q) { return ((uintptr_t)q & 15) == 0; }
 
-pt_status launch_gn(pt_ctx *c, GnP p, GnArgs a, int mode, int act, cudaStream_t st)
+struct GnPlan {
+    GnP key, p;                  // what gn_params gave, and with the launch shape
+    int mode;                    // the kernel's number
+    size_t smem;
+};
+typedef std::unordered_multimap<uint64_t, GnPlan> GnPlans;
+
+void gn_config(cudaLaunchConfig_t *cfg, cudaLaunchAttribute (&attr)[2], int clusters, int cl, int threads, size_t smem, cudaStream_t st)
 {
-    const bool res = a.res != nullptr;
-    const GnKernel kernel = gn_kernel_of(mode, act, res);
-    const unsigned bit = 1u << ((mode * 3 + act) * 2 + (res ? 1 : 0));
-    if (!(c->gn_attr_done & bit)) {
-        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 * 1024));
-        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-        c->gn_attr_done |= bit;
-    }
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    memset(&cfg, 0, sizeof(cfg));
+    memset(cfg, 0, sizeof(*cfg));
+    memset(attr, 0, sizeof(attr));
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    // the cluster size of the least estimated time
-    double best = 1e30;
-    int best_cl = 0, best_n = 0;
-    for (int cl = 1; cl <= kGnMaxCluster; cl *= 2) {
-        if (cl > 1 && (cl > p.HW || cl * p.G > kGnExchange)) break;
-        GnP q = p;
-        const size_t smem = gn_shape(&q, mode, res, cl);
-        if (smem > 225 * 1024) continue;
-        cfg.gridDim = dim3((unsigned)cl); cfg.blockDim = dim3((unsigned)q.threads); cfg.dynamicSmemBytes = smem;
-        attr[1].val.clusterDim.x = (unsigned)cl;
+    attr[1].val.clusterDim.x = (unsigned)cl; attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg->gridDim = dim3((unsigned)(clusters * cl)); cfg->blockDim = dim3((unsigned)threads); cfg->dynamicSmemBytes = smem; cfg->stream = st;
+    cfg->attrs = attr;
+    cfg->numAttrs = cl > 1 ? 2 : 1;
+}
+
+// Clusters of cl blocks that the device holds at once, with shared memory for two blocks on an SM or for one.
+pt_status gn_fit(pt_ctx *c, GnKernel kernel, int index, int cl, bool two, int *n)
+{
+    int &known = c->gn_fit[index][cl][two ? 1 : 0];
+    if (!known) {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[2];
+        int m = 0;
+        gn_config(&cfg, attr, 1, cl, kGnThreads, two ? kGnSmem : kGnSmemMost, nullptr);
         cfg.numAttrs = 2;
-        int n = 0;
-        if (cl > 1) {
-            PT_CUDA_OK(cudaOccupancyMaxActiveClusters(&n, (const void *)kernel, &cfg));
-        } else {
-            PT_CUDA_OK(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)kernel, (int)cfg.blockDim.x, smem));
-            n *= c->sm_count;
-        }
-        if (n < 1) continue;
-        if (n > kGnBlocks * c->sm_count) n = kGnBlocks * c->sm_count;
-        const int clusters = n < p.N ? n : p.N, waves = pt_ceil_div(p.N, clusters);
-        const double slot = gn_slot(mode, res), in = (double)q.share * p.LV * slot, ring = (double)kGnThreads * kGnRows * gn_batches(mode, res) * slot;
-        const double bytes = in + 2.0 * q.share * p.ld + 0.5 * (in > ring ? in - ring : 0.0);
-        double rate = 6500e3 / (clusters * cl);                   // bytes per microsecond and block
-        if (rate > 60e3) rate = 60e3;
-        const double us = waves * (bytes / rate + 2.0 + (cl > 1 ? 0.5 : 0.0));
-        if (us < best) { best = us; best_cl = cl; best_n = clusters; }
+        PT_CUDA_OK(cudaOccupancyMaxActiveClusters(&m, (const void *)kernel, &cfg));
+        known = m + 1;
     }
-    if (!best_cl) return PT_ERR_UNSUPPORTED;
-    const size_t smem = gn_shape(&p, mode, res, best_cl);
-    p.clusters = best_n;
-    cfg.gridDim = dim3((unsigned)(p.clusters * p.cl)); cfg.blockDim = dim3((unsigned)p.threads); cfg.dynamicSmemBytes = smem;
-    attr[1].val.clusterDim.x = (unsigned)p.cl;
-    cfg.numAttrs = p.cl > 1 ? 2 : 1;
+    *n = known - 1;
+    return PT_OK;
+}
+
+// The slabs and the cluster size of the least estimated time. A unit of work costs a block about 4.5 us whatever it holds (loads, barriers,
+// exchange, all in a row), so that one unit per block is best nearly everywhere, and r per row of its threads. Microseconds by clusters of
+// 1, 2, 4, 8, 16 blocks: 183, 99, 88, 98, 126 for the backward pass at 64x56x56x256 (64 images; four slabs without clusters: 85), 48.5, 33.8,
+// 28.5, 34.4, 57.5 for the forward pass at 64x28x28x371; 92, 50, 29, 18, 13 at 2x112x112x64, and 9.4 with four slabs and 9 blocks.
+pt_status gn_plan(pt_ctx *c, GnKernel kernel, int index, int mode, bool res, GnPlan *plan)
+{
+    const bool blocks = mode == kGnFwdPack || mode == kGnBwdPacked;
+    const double row = (mode == kGnFwd ? 0.25 : mode == kGnFwdPack ? 0.4 : mode == kGnBwd ? 0.45 : 0.55) + (res ? 0.1 : 0.0);
+    double best = 1e30;
+    int last = 0;
+    for (int want = 1; want <= kGnSlabs && want <= plan->key.G; ++want) {
+        GnP q = plan->key;
+        gn_slabs(&q, want, blocks);
+        if (q.slabs == last) continue;
+        last = q.slabs;
+        if (q.slabs > 1 && q.rl < 2) break;                              // (a slab of 16 bytes a pixel would read every sector twice)
+        for (int cl = 1; cl <= kGnMaxCluster; ++cl) {
+            if (cl > 1 && (cl > q.HW || cl * q.gs > kGnExchange)) break;
+            GnP r = q;
+            const size_t smem = gn_shape(&r, mode, res, cl);
+            if (smem > kGnSmemMost) continue;
+            int n = 0;
+            const pt_status s = gn_fit(c, kernel, index, cl, smem <= kGnSmem, &n);
+            if (s != PT_OK) return s;
+            if (n < 1) continue;
+            const int most = (smem <= kGnSmem ? kGnBlocks : 1) * c->sm_count / cl, units = q.N * q.slabs;
+            n = n < most ? n : most;
+            r.clusters = n < units ? n : units;
+            const bool shared = r.clusters * cl > c->sm_count;
+            const double rows = (double)pt_ceil_div(r.share, r.ppb) * r.threads / kGnThreads, narrow = q.rl < 4 && q.slabs > 1 ? 1.25 : 1.0;
+            const double us = pt_ceil_div(units, r.clusters) * (4.5 + rows * row * narrow * (shared ? 1.8 : 1.0)) + (cl > 1 ? 0.7 : 0.0) + (shared ? 1.0 : 0.0);
+            if (us < best) { best = us; plan->p = r; plan->smem = smem; }
+        }
+    }
+    return best < 1e30 ? PT_OK : PT_ERR_UNSUPPORTED;
+}
+
+// The plan of a shape: those met so far are kept, choosing one walks a few hundred candidates.
+pt_status gn_plan_of(pt_ctx *c, GnKernel kernel, int index, int mode, bool res, const GnP &key, GnPlan *plan)
+{
+    uint64_t h = (uint64_t)index, w;
+    for (size_t k = 0; k + 8 <= sizeof(GnP); k += 8) {
+        memcpy(&w, reinterpret_cast<const char *>(&key) + k, 8);
+        h = (h ^ w) * 0x9e3779b97f4a7c15ull;
+        h ^= h >> 29;
+    }
+    std::lock_guard<std::mutex> lock(c->gn_mutex);
+    GnPlans *known = static_cast<GnPlans *>(c->gn_plans.get());
+    if (known) {
+        const auto range = known->equal_range(h);
+        for (auto it = range.first; it != range.second; ++it)
+            if (it->second.mode == index && memcmp(&it->second.key, &key, sizeof(GnP)) == 0) {
+                *plan = it->second;
+                return PT_OK;
+            }
+    }
+    memset(plan, 0, sizeof(*plan));
+    memcpy(&plan->key, &key, sizeof(GnP));
+    plan->mode = index;
+    const pt_status r = gn_plan(c, kernel, index, mode, res, plan);
+    if (r != PT_OK) return r;
+    try {
+        if (!known) {
+            c->gn_plans = std::make_shared<GnPlans>();
+            known = static_cast<GnPlans *>(c->gn_plans.get());
+        }
+        if (known->size() >= pt_ctx::kGnPlans) known->clear();
+        known->emplace(h, *plan);
+    } catch (const std::bad_alloc &) {                           // (no room: the plan is chosen again next time)
+    }
+    return PT_OK;
+}
+
+pt_status launch_gn(pt_ctx *c, const GnP &key, const GnArgs &a, int mode, int act, cudaStream_t st)
+{
+    const bool res = a.res != nullptr;
+    const GnKernel kernel = gn_kernel_of(mode, act, res);
+    const int index = (mode * 3 + act) * 2 + (res ? 1 : 0);
+    if (!(c->gn_attr_done & (1u << index))) {
+        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGnSmemMost));
+        PT_CUDA_OK(cudaFuncSetAttribute((const void *)kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        c->gn_attr_done |= 1u << index;
+    }
+    GnPlan plan;
+    const pt_status r = gn_plan_of(c, kernel, index, mode, res, key, &plan);
+    if (r != PT_OK) return r;
+    const GnP &p = plan.p;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    gn_config(&cfg, attr, p.clusters, p.cl, p.threads, plan.smem, st);
     PT_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, p, a));
     c->launches += 1;
-    if (mode >= kGnBwd && p.clusters > 1) {
-        PT_CUDA_OK(pt_launch_pdl(gn_finish_kernel, dim3((unsigned)pt_ceil_div(2 * p.ld, 32)), dim3(1024), 0, st, (const double *)a.rows, p.clusters, p.C,
+    if (mode >= kGnBwd && p.clusters * p.cl > 1) {
+        PT_CUDA_OK(pt_launch_pdl(gn_finish_kernel, dim3((unsigned)pt_ceil_div(2 * p.ld, 32)), dim3(1024), 0, st, (const float *)a.rows, p.clusters * p.cl, p.C,
                                  p.ld, a.dgamma, a.dbeta));
         c->launches += 1;
     }
@@ -888,9 +1030,8 @@ extern "C" size_t pt_gn_workspace_bytes(const pt_ctx *c, const pt_gn_desc *d)
 {
     GnP p;
     if (gn_params(c, d, false, &p) != PT_OK) return 0;
-    // a row of sums per cluster: no more than there are images, or blocks on the device
-    const size_t most = (size_t)c->sm_count * 2;
-    return ((size_t)p.N < most ? (size_t)p.N : most) * 2 * p.ld * sizeof(double);
+    // a row of sums per block
+    return (size_t)c->sm_count * kGnBlocks * 2 * p.ld * sizeof(float);
 }
 
 extern "C" pt_status pt_gn_act_fwd(pt_ctx *c, const pt_gn_desc *d, const void *x, const void *residual, const float *gamma, const float *beta,
@@ -920,7 +1061,7 @@ extern "C" pt_status pt_gn_act_bwd(pt_ctx *c, const pt_gn_desc *d, const void *x
     GnArgs a{};
     a.x = (const uint4 *)x; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy; a.gamma = gamma; a.beta = beta; a.mean = save_mean;
     a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual;
-    a.rows = (double *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.rows = (float *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
     return launch_gn(c, p, a, kGnBwd, d->act, (cudaStream_t)stream);
 }
 
@@ -938,6 +1079,6 @@ extern "C" pt_status pt_gn_act_bwd_packed(pt_ctx *c, const pt_gn_desc *d, const 
     GnArgs a{};
     a.codes_in = (const uint8_t *)codes; a.scales_in = (const uint8_t *)scales; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy;
     a.gamma = gamma; a.beta = beta; a.mean = save_mean; a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual; a.y = (uint4 *)y;
-    a.rows = (double *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.rows = (float *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
     return launch_gn(c, p, a, kGnBwdPacked, d->act, (cudaStream_t)stream);
 }

@@ -5,6 +5,7 @@
 #include <stdint.h>
 #include <string.h>
 #include <atomic>
+#include <memory>
 #include <mutex>
 #include <unordered_map>
 #include <vector>
@@ -71,7 +72,13 @@ struct pt_ctx {
     int device = 0;
     int sm_count = 0;
     mutable std::atomic<unsigned> attr_done{0};
-    mutable std::atomic<unsigned> gn_attr_done{0};            // the same for the group-norm kernels
+    mutable std::atomic<unsigned> gn_attr_done{0};      // the same for the group-norm kernels
+    // Group norm: clusters that the device holds at once, by kernel, cluster size and blocks of an SM (plus one; 0: not asked yet), and the
+    // launch shapes of the descriptors met so far (pt_gn.cu's type; past kGnPlans the table starts again)
+    int gn_fit[24][17][2] = {};
+    std::shared_ptr<void> gn_plans;
+    std::mutex gn_mutex;
+    static constexpr size_t kGnPlans = 2048;
     int cc_major = 0, cc_minor = 0;
     unsigned int *d_status = nullptr;   // 4 words, device
     unsigned int *h_status = nullptr;   // 4 words, pinned host
