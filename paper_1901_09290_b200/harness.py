@@ -578,10 +578,15 @@ class ChainedStep:
     Block structure is read from the layer names: "stem", then "<block>.c1", "<block>.c2", ... and an optional "<block>.ds"
     (projection shortcut) per block, in order."""
 
+    keeps_tensors = True                                   # every tensor of a step has a buffer of its own
+
     def __init__(self, ctx: B.Context, net: W.Net, N: int, seed: int, fused_stats: bool = True, algo: int = 0,
                  max_blocks: Optional[int] = None, model: Optional[W.Model] = None, x0: Optional[torch.Tensor] = None,
-                 g_last: Optional[torch.Tensor] = None, wgrad_streams: int = 0):
-        self.ctx, self.net, self.N, self.fused = ctx, net, N, fused_stats
+                 g_last: Optional[torch.Tensor] = None, wgrad_streams: int = 0, norm: str = "batch", groups: int = 32):
+        if norm not in ("batch", "group"):
+            raise ValueError(f"norm is 'batch' or 'group', not {norm!r}")
+        self.ctx, self.net, self.N, self.fused = ctx, net, N, fused_stats and norm == "batch"
+        self.norm, self.groups = norm, groups
         # wgrad_streams > 0: a layer's weight gradient needs only its input and dy, so it goes to a side stream (round robin,
         # a workspace each) and runs beside the rest of the backward chain; the launches are held to SMs / streams CTAs so
         # that the split ones, whose CTAs wait for one another, always fit on the device together
@@ -626,12 +631,14 @@ class ChainedStep:
             ldx = self.ld_img if i == 0 else W.pad16(l.C)
             self.desc[i] = B.make_conv_desc(N, l.H, l.H, l.C, l.K, l.R, l.R, l.stride, l.pad, ldx, self.ld[i], W.pad8(l.C), 0, algo)
             self.bn_desc[i] = None
-            self.y[i] = bf(N, l.P, self.ld[i])             # convolution output
-            self.a[i] = bf(N, l.P, self.ld[i])             # after normalisation (+ residual) (+ ReLU)
-            self.dy[i] = bf(N, l.P, self.ld[i])            # gradient with respect to the convolution output
+            if self.keeps_tensors:
+                self.y[i] = bf(N, l.P, self.ld[i])         # convolution output
+                self.a[i] = bf(N, l.P, self.ld[i])         # after normalisation (+ residual) (+ ReLU)
+                self.dy[i] = bf(N, l.P, self.ld[i])        # gradient with respect to the convolution output
             self.gamma[i] = (torch.rand(l.K, generator=gen) + 0.5).cuda()
             self.beta[i] = (torch.rand(l.K, generator=gen) - 0.5).cuda()
-            self.sm[i], self.si[i] = torch.empty(l.K, device=dev), torch.empty(l.K, device=dev)
+            stats = (l.K,) if norm == "batch" else (N, min(groups, l.K))
+            self.sm[i], self.si[i] = torch.empty(stats, device=dev), torch.empty(stats, device=dev)
             self.dg[i], self.db[i] = torch.empty(l.K, device=dev), torch.empty(l.K, device=dev)
             for which in range(3):
                 ws_conv = max(ws_conv, B.pt_conv_workspace_bytes(ctx, self.desc[i], which))
@@ -641,8 +648,13 @@ class ChainedStep:
         for i in self.used:
             l = L[i]
             relu = i not in ds_set                         # the projection shortcut is normalised but not rectified
-            self.bn_desc[i] = B.make_bn_desc(N, l.P, l.P, l.K, self.ld[i], 1e-5, 0.1, relu)
-            ws_bn = max(ws_bn, B.pt_bn_workspace_bytes(ctx, self.bn_desc[i]))
+            if norm == "batch":
+                self.bn_desc[i] = B.make_bn_desc(N, l.P, l.P, l.K, self.ld[i], 1e-5, 0.1, relu)
+                ws_bn = max(ws_bn, B.pt_bn_workspace_bytes(ctx, self.bn_desc[i]))
+            else:
+                begin = W.group_begin(l.K, groups)
+                self.bn_desc[i] = B.make_gn_desc(N, l.P, l.P, l.K, len(begin) - 1, self.ld[i], 1e-5, B.PT_ACT_RELU if relu else B.PT_ACT_NONE, begin)
+                ws_bn = max(ws_bn, B.pt_gn_workspace_bytes(ctx, self.bn_desc[i]))
         self.last_of = last_of
         self.ws = torch.empty(ws_conv, dtype=torch.uint8, device=dev)
         self.ws_side = [torch.empty(ws_conv, dtype=torch.uint8, device=dev) for _ in range(max(0, wgrad_streams))]
@@ -662,11 +674,11 @@ class ChainedStep:
             self.d_pooled = bf(N, first_h, self.ld[0])
         # gradients with respect to activations: one buffer per distinct activation a convolution reads
         # gradient with respect to a convolution's INPUT (its data gradient), and with respect to the stem's activation
-        self.da = {i: bf(N, L[i].H, W.pad16(L[i].C)) for i in self.used if i != 0}
-        self.d_a0 = bf(N, l0.P, self.ld[0])
+        self.da = {i: bf(N, L[i].H, W.pad16(L[i].C)) for i in self.used if i != 0 and self.keeps_tensors}
+        self.d_a0 = bf(N, l0.P, self.ld[0]) if self.keeps_tensors else None
         self.da_tmp = {}
         self.dres = {}
-        for main, ds, _ in self.blocks:
+        for main, ds, _ in self.blocks if self.keeps_tensors else ():
             lo = L[main[-1]]
             self.dres[main[-1]] = bf(N, lo.P, self.ld[main[-1]])             # gradient handed to the residual branch
         out_i = self.blocks[-1][0][-1] if self.blocks else 0
@@ -697,6 +709,9 @@ class ChainedStep:
                                    self.a[i], stats, n_parts, stream)
         else:
             B.pt_conv_fwd(c, self.desc[i], x, self.dm.wb[i], self.y[i], ws, stream)
+            if self.norm == "group":
+                B.pt_gn_act_fwd(c, self.bn_desc[i], self.y[i], residual, self.gamma[i], self.beta[i], self.sm[i], self.si[i], self.a[i], stream=stream)
+                return self.a[i]
             B.pt_bn_relu_fwd(c, self.bn_desc[i], self.y[i], residual, self.gamma[i], self.beta[i], None, None, self.sm[i], self.si[i],
                              self.a[i], ws_bn, stream)
         return self.a[i]
@@ -725,7 +740,11 @@ class ChainedStep:
             cur = self._conv_bn(main[-1], t, res, stream)
         return cur
 
-    def _bn_bwd(self, i, d_out, dres, stream=None, aux=False):
+    def _bn_bwd(self, i, d_out, dres, stream=None, aux=False, residual=None):
+        if self.norm == "group":
+            B.pt_gn_act_bwd(self.ctx, self.bn_desc[i], self.y[i], residual, d_out, self.gamma[i], self.beta[i], self.sm[i], self.si[i], self.dy[i],
+                            dres, self.dg[i], self.db[i], self.ws_bn_aux if aux else self.ws_bn, stream)
+            return
         B.pt_bn_relu_bwd(self.ctx, self.bn_desc[i], self.y[i], self.a[i], d_out, self.gamma[i], self.sm[i], self.si[i], self.dy[i], dres,
                          self.dg[i], self.db[i], self.ws_bn_aux if aux else self.ws_bn, stream)
 
@@ -750,7 +769,7 @@ class ChainedStep:
             main, ds, _ = self.blocks[bi]
             x_in = self.block_in[bi]
             last = main[-1]
-            self._bn_bwd(last, d_cur, self.dres[last], stream)
+            self._bn_bwd(last, d_cur, self.dres[last], stream, residual=self.a[ds] if ds is not None else x_in)
             ms = stream if stream is not None else torch.cuda.current_stream()
             side = self._aux if ds is not None else None
             if side is not None:
@@ -812,3 +831,122 @@ class ChainedStep:
             fl = 2 * self.N * l.P * l.P * l.K * l.C * l.R * l.R
             f += (2 if i == 0 else 3) * fl
         return f
+
+
+class CheckpointedStep(ChainedStep):
+    """The chain with group normalisation that keeps its activations in 8 bits between the passes. A layer keeps the checkpoint of its
+    convolution's output and nothing else: the backward pass of its normalisation restores the activation that the next convolution's
+    weight gradient reads. Blocks keep the checkpoints of their input and, behind a projection, of the shortcut. Convolution outputs and
+    activations live in a few buffers that all layers share."""
+
+    keeps_tensors = False
+
+    def __init__(self, ctx: B.Context, net: W.Net, N: int, seed: int, groups: int = 32, algo: int = 0, max_blocks: Optional[int] = None,
+                 model: Optional[W.Model] = None, x0: Optional[torch.Tensor] = None, g_last: Optional[torch.Tensor] = None):
+        self._shared = {}
+        super().__init__(ctx, net, N, seed, False, algo, max_blocks, model, x0, g_last, 0, "group", groups)
+        L = net.layers
+        self.ck = {i: B.checkpoint_buffers(N * L[i].P ** 2, L[i].K) for i in self.used}
+        # the blocks' inputs, and the shortcuts behind a projection: descriptor and checkpoint
+        def saved(P, K, ld):
+            return (B.make_pack_desc(N * P * P, K, ld),) + B.checkpoint_buffers(N * P * P, K)
+        self.in_ck = [saved(L[m[0]].H, L[m[0]].C, W.pad16(L[m[0]].C)) for m, _, _ in self.blocks]
+        self.ds_ck = [saved(L[d].P, L[d].K, self.ld[d]) if d is not None else None for _, d, _ in self.blocks]
+
+    def _buffer(self, name, shape):
+        """A view of the shared buffer `name`. Each has room for the network's largest activation from the start."""
+        if name not in self._shared:
+            L = self.net.layers
+            most = max(max(self.N * L[i].P ** 2 * self.ld[i], self.N * L[i].H ** 2 * W.pad16(L[i].C) if i else 0) for i in self.used)
+            self._shared[name] = torch.zeros(most, dtype=torch.bfloat16, device="cuda")
+        n = 1
+        for s in shape:
+            n *= s
+        return self._shared[name][:n].view(shape)
+
+    def _shape(self, i):
+        P = self.net.layers[i].P
+        return self.N, P, P, self.ld[i]
+
+    def _layer(self, i, x, residual, out, stream):
+        """Convolution and normalisation of layer i into the shared buffer `out`; leaves the layer's checkpoint."""
+        y, a = self._buffer("y", self._shape(i)), self._buffer(out, self._shape(i))
+        B.pt_conv_fwd(self.ctx, self.desc[i], x, self.dm.wb[i], y, self.ws, stream)
+        B.pt_gn_act_fwd(self.ctx, self.bn_desc[i], y, residual, self.gamma[i], self.beta[i], self.sm[i], self.si[i], a, *self.ck[i], stream)
+        return a
+
+    def forward(self, stream=None):
+        c = self.ctx
+        cur = self._layer(0, self.x0, None, "a0", stream)
+        if self.pool:
+            B.pt_maxpool_fwd(c, self.pool_desc, cur, self.pooled, stream, index=self.pool_index)
+            cur = self.pooled
+        for b, (main, ds, _) in enumerate(self.blocks):
+            B.pt_act_pack(c, self.in_ck[b][0], cur, *self.in_ck[b][1:], stream)
+            res = cur
+            if ds is not None:
+                res = self._layer(ds, cur, None, "shortcut", stream)
+                B.pt_act_pack(c, self.ds_ck[b][0], res, *self.ds_ck[b][1:], stream)
+            t = cur
+            for k, i in enumerate(main[:-1]):
+                t = self._layer(i, t, None, "t%d" % (k & 1), stream)
+            cur = self._layer(main[-1], t, res, "out%d" % (b & 1), stream)
+        return cur
+
+    def _norm_bwd(self, i, residual, d_out, dres, y, dy, stream):
+        dy = self._buffer(dy, self._shape(i))
+        B.pt_gn_act_bwd_packed(self.ctx, self.bn_desc[i], *self.ck[i], residual, d_out, self.gamma[i], self.beta[i], self.sm[i], self.si[i], dy, dres,
+                               self.dg[i], self.db[i], y, self.ws_bn, stream)
+        return dy
+
+    def _filters(self, i, x, dy, stream):
+        B.pt_conv_wgrad(self.ctx, self.desc[i], x, dy, self.dm.g[i], self.ws, stream)
+
+    def _input_grad(self, i, dy, out, stream):
+        l = self.net.layers[i]
+        dx = self._buffer(out, (self.N, l.H, l.H, W.pad16(l.C)))
+        B.pt_conv_dgrad(self.ctx, self.desc[i], dy, self.dm.wb[i], dx, self.ws, stream)
+        return dx
+
+    def backward(self, stream=None):
+        c, L = self.ctx, self.net.layers
+        d_cur = self.g_last
+        for b in range(len(self.blocks) - 1, -1, -1):
+            main, ds, _ = self.blocks[b]
+            li, last = L[main[0]], main[-1]
+            x_in = self._buffer("x_in", (self.N, li.H, li.H, W.pad16(li.C)))
+            B.pt_act_unpack(c, self.in_ck[b][0], *self.in_ck[b][1:], x_in, stream)
+            res = x_in
+            if ds is not None:
+                res = self._buffer("shortcut", self._shape(ds))
+                B.pt_act_unpack(c, self.ds_ck[b][0], *self.ds_ck[b][1:], res, stream)
+            dres = self._buffer("dres", self._shape(last))
+            dy = self._norm_bwd(last, res, d_cur, dres, None, "dy%d" % (len(main) & 1), stream)
+            for k in range(len(main) - 1, -1, -1):
+                d_t = self._input_grad(main[k], dy, "d%d" % (k & 1), stream)
+                if k == 0:
+                    self._filters(main[0], x_in, dy, stream)
+                    break
+                # the filters' gradient waits for the activation that the layer before restores
+                x = self._buffer("t0", self._shape(main[k - 1]))
+                before = self._norm_bwd(main[k - 1], None, d_t, None, x, "dy%d" % (k & 1), stream)
+                self._filters(main[k], x, dy, stream)
+                dy = before
+            sc = dres
+            if ds is not None:
+                dy = self._norm_bwd(ds, None, dres, None, None, "dy0", stream)
+                self._filters(ds, x_in, dy, stream)
+                sc = self._input_grad(ds, dy, "d_shortcut", stream)
+            total = self._buffer("sum%d" % (b & 1), d_t.shape)
+            self._add(d_t, sc, total, li.C, W.pad16(li.C), self.N * li.H * li.H, stream)
+            d_cur = total
+        if self.pool:
+            d_a0 = self._buffer("d0", self._shape(0))
+            B.pt_maxpool_bwd(c, self.pool_desc, None, d_cur, d_a0, stream, index=self.pool_index)
+            d_cur = d_a0
+        self._filters(0, self.x0, self._norm_bwd(0, None, d_cur, None, None, "dy0", stream), stream)
+
+    def saved_bytes(self) -> int:
+        """What stays between the forward and the backward pass of a step: the checkpoints and the statistics."""
+        pairs = list(self.ck.values()) + [s[1:] for s in self.in_ck + self.ds_ck if s is not None]
+        return sum(t.numel() for p in pairs for t in p) + sum(t.numel() * 4 for d in (self.sm, self.si) for t in d.values())

@@ -3,6 +3,7 @@
     python -m paper_1901_09290_b200.layerbench --layer s1b1.c3 --passes fwd,dgrad,wgrad --iters 20
     python -m paper_1901_09290_b200.layerbench --shape 64,56,36,143,1,1 --passes fwd      # N,H,C,K,R,stride
     python -m paper_1901_09290_b200.layerbench --bn 64,56,143                              # batch norm + ReLU + residual: N,H,C
+    python -m paper_1901_09290_b200.layerbench --gn 64,28,371,32 --act silu                # group norm, and from 8-bit checkpoints: N,H,C,groups
     python -m paper_1901_09290_b200.layerbench --model --iters 5      # lasso step, detection, compaction of the whole model alone
 
 It is also the small case ncu captures are taken on.
@@ -61,6 +62,9 @@ def main():
     ap.add_argument("--wgrad-ctas", type=int, default=0, help="CTA limit of the weight-gradient kernels (0 = one per SM)")
     ap.add_argument("--no-graph", action="store_true", help="time eager launches (includes host launch cost)")
     ap.add_argument("--bn", default=None, help="N,H,C: time pt_bn_relu_fwd / pt_bn_relu_bwd instead of a convolution")
+    ap.add_argument("--gn", default=None, help="N,H,C,groups: time the group norm's passes, with and without checkpoints, and the checkpoints alone")
+    ap.add_argument("--act", default="relu", choices=["none", "relu", "silu"], help="activation of --gn")
+    ap.add_argument("--residual", action="store_true", help="--gn with a residual add")
     ap.add_argument("--gate", default=None, help="N,H,C,S: time pt_channel_gather / pt_channel_scatter_add of S of a node's C channels")
     ap.add_argument("--stats", action="store_true",
                     help="the forward pass through pt_conv_fwd_stats (batch-norm statistics taken in the epilogue)")
@@ -74,6 +78,8 @@ def main():
         return gate_main(args)
     if args.bn:
         return bn_main(args)
+    if args.gn:
+        return gn_main(args)
     if args.shape:
         N, H, C, K, R, stride = [int(t) for t in args.shape.split(",")]
         name = args.shape
@@ -182,6 +188,55 @@ def bn_main(args):
         torch.cuda.synchronize()
         us = e0.elapsed_time(e1) * 1e3 / args.iters
         by = elems * (6 if ps == "fwd" else 10)
+        out[ps] = {"us": round(us, 2), "gbs": round(by / us / 1e3, 1)}
+    ctx.poll()
+    print(json.dumps(out))
+
+
+def gn_main(args):
+    """Group norm (+ residual) + activation on one activation tensor: device time and algorithmic GB/s, every tensor counted once."""
+    N, H, C, G = [int(t) for t in args.gn.split(",")]
+    act = {"none": B.PT_ACT_NONE, "relu": B.PT_ACT_RELU, "silu": B.PT_ACT_SILU}[args.act]
+    ld, npix, begin = W.pad16(C), N * H * H, W.group_begin(C, G)
+    G = len(begin) - 1
+    ctx = B.Context(0)
+    d, pd = B.make_gn_desc(N, H, H, C, G, ld, act=act, group_begin=begin), B.make_pack_desc(npix, C, ld)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    mk = lambda: torch.randn((N, H, H, ld), generator=g, device="cuda").to(torch.bfloat16)
+    sets = [dict(x=mk(), r=mk() if args.residual else None, y=mk(), dy=mk(), dx=mk(), dr=mk() if args.residual else None,
+                 ck=B.checkpoint_buffers(npix, C)) for _ in range(args.sets)]
+    gamma, beta = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    mean, rstd = (torch.zeros((N, G), device="cuda") for _ in range(2))
+    dg, db = (torch.empty(C, device="cuda") for _ in range(2))
+    ws = torch.empty(B.pt_gn_workspace_bytes(ctx, d), dtype=torch.uint8, device="cuda")
+    elems, code = npix * C, npix * (C + (C + 31) // 32)
+    res = 2 * elems if args.residual else 0
+    passes = {
+        "fwd": (lambda s: B.pt_gn_act_fwd(ctx, d, s["x"], s["r"], gamma, beta, mean, rstd, s["y"]), 4 * elems + res),
+        "fwd_packed": (lambda s: B.pt_gn_act_fwd(ctx, d, s["x"], s["r"], gamma, beta, mean, rstd, s["y"], *s["ck"]), 4 * elems + res + code),
+        "bwd": (lambda s: B.pt_gn_act_bwd(ctx, d, s["x"], s["r"], s["dy"], gamma, beta, mean, rstd, s["dx"], s["dr"], dg, db, ws), 6 * elems + 2 * res),
+        "bwd_packed": (lambda s: B.pt_gn_act_bwd_packed(ctx, d, *s["ck"], s["r"], s["dy"], gamma, beta, mean, rstd, s["dx"], s["dr"], dg, db, s["y"], ws),
+                       code + 6 * elems + 2 * res),
+        "pack": (lambda s: B.pt_act_pack(ctx, pd, s["x"], *s["ck"]), 2 * elems + code),
+        "unpack": (lambda s: B.pt_act_unpack(ctx, pd, *s["ck"], s["y"]), 2 * elems + code),
+    }
+    out = {"gn": args.gn, "act": args.act, "ld": ld}
+    for ps, (run, by) in passes.items():
+        for i in range(3):
+            run(sets[i % len(sets)])
+        torch.cuda.synchronize()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            for i in range(args.iters):
+                run(sets[i % len(sets)])
+        gr.replay()
+        torch.cuda.synchronize()
+        e0.record()
+        gr.replay()
+        e1.record()
+        torch.cuda.synchronize()
+        us = e0.elapsed_time(e1) * 1e3 / args.iters
         out[ps] = {"us": round(us, 2), "gbs": round(by / us / 1e3, 1)}
     ctx.poll()
     print(json.dumps(out))

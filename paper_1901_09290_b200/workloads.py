@@ -341,6 +341,24 @@ def layer_seed(cfg_index: int, layer_index: int, what: int = 0) -> int:
     return BASE_SEED + cfg_index + 1000 * layer_index + 100000 * what
 
 
+def group_begin(C: int, groups: int) -> List[int]:
+    """First channels of at most `groups` groups of C channels, and C: equal groups where C is a multiple, else as equal as whole
+    channels allow (a pruned layer's count is hardly ever a multiple)."""
+    groups = min(groups, C)
+    return [g * C // groups for g in range(groups + 1)]
+
+
+def pruned_group_begin(kept: Sequence[int], begin: Sequence[int]) -> List[int]:
+    """The groups that a reconfiguration leaves: the kept channels (ascending, in the old numbering) stay with their group, and groups
+    without a kept channel go."""
+    out = [0]
+    for s, e in zip(begin[:-1], begin[1:]):
+        n = sum(1 for k in kept if s <= k < e)
+        if n:
+            out.append(out[-1] + n)
+    return out
+
+
 def pad8(c: int) -> int:
     """Smallest legal channel pitch: the next multiple of 8 elements (16 bytes of bf16)."""
     return (int(c) + 7) // 8 * 8
