@@ -501,6 +501,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         };
         // the ring's places in the order of the walk, and where they begin and end
         const uint32_t s_first = dir ? (B - 1) * kPlace : 0u, s_last = dir ? 0u : (B - 1) * kPlace, s_step = dir ? 0u - kPlace : kPlace;
+        const uint4 keep_own = lane_ok ? keep : make_uint4(0u, 0u, 0u, 0u);
         uint32_t s = s_first;
         Pos here = src.at, then = moved(src.at, B);
         for (int b = 0; b < NB; ++b) {
@@ -508,21 +509,40 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             const bool all = b < full;
             if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
                 uint8_t *gq = a.codes + base * p.ldq + (size_t)b * step_q, *gs = a.scales + base * p.nb + (size_t)b * step_s;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const bool ok = all || u * p.ppb < tail;
-                    Raw w;
-                    w.x = make_uint4(0u, 0u, 0u, 0u);
-                    if (ok) {
-                        fetch(w, here.s, s, u);
-                        count(w);
-                    }
-                    w.x = act8::and4(w.x, keep);
-                    if (!lane_ok) w.x = make_uint4(0u, 0u, 0u, 0u);
-                    const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(w.x), p.w));
-                    if (ok && lane_ok && has) {
+                const auto store = [&](const Raw &w, uint32_t byte, int u) {
+                    if (lane_ok && has) {
                         *reinterpret_cast<uint2 *>(gq + (uint32_t)(pr * p.ldq + c0 + u * (int)row_q)) = act8::encode8(w.x, byte);
                         if ((cv & 3) == 0) gs[(uint32_t)(pr * p.nb + (cv >> 2) + u * (int)row_s)] = (uint8_t)byte;
+                    }
+                };
+                if (all) {
+                    Raw w[U];
+                    uint32_t top[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) fetch(w[u], here.s, s, u);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        count(w[u]);
+                        w[u].x = act8::and4(w[u].x, keep_own);
+                        top[u] = act8::amax8(w[u].x);
+                    }
+#pragma unroll
+                    for (int u = 0; u < U; ++u) top[u] = act8::scale_byte(act8::block_max(top[u], p.w));
+#pragma unroll
+                    for (int u = 0; u < U; ++u) store(w[u], top[u], u);
+                } else {
+#pragma unroll 1
+                    for (int u = 0; u < U; ++u) {
+                        const bool ok = u * p.ppb < tail;
+                        Raw w;
+                        w.x = make_uint4(0u, 0u, 0u, 0u);
+                        if (ok) {
+                            fetch(w, here.s, s, u);
+                            count(w);
+                        }
+                        w.x = act8::and4(w.x, keep_own);
+                        const uint32_t byte = act8::scale_byte(act8::block_max(act8::amax8(w.x), p.w));
+                        if (ok) store(w, byte, u);
                     }
                 }
             } else if (all) {                                            // a batch at a time, its loads first
