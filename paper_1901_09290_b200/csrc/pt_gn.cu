@@ -41,11 +41,12 @@ constexpr int kGnBlocks = 2;                 // blocks of an SM: while one excha
 constexpr size_t kGnSmem = 113 * 1024, kGnSmemMost = 226 * 1024;     // shared memory of a block: two on an SM, one
 
 struct GnP {
-    int N, HW, C, ld, LV, ldq, nb, G;
+    int N, HW, C, ld, LV, ldq, nb, G, cg;        // (cg: channels of a group without a table)
     int slabs, gs;               // slabs of channels, most groups of one; a unit of work is an image's slab
     int w, rl, ppb, threads;     // lanes of a checkpoint's block, lanes of a pixel, pixels the threads cover at a time, threads
-    int gl, gc;                  // lanes that add up a group, and those of them that take different channels
+    int gl, gc;                  // lanes that add up a group, and those of them that take different channels (as powers of two)
     int cl, clusters, share;     // blocks of a cluster, clusters, pixels of a block
+    int step_n, step_s;          // a cluster's next unit: images and slabs further on
     int table;
     unsigned sm_gid, sm_gam, sm_bet, sm_grp, sm_red, sm_xch, sm_acc, sm_ring;
     float eps;
@@ -64,7 +65,7 @@ struct GnArgs {
     float *dgamma, *dbeta;
 };
 
-__device__ __forceinline__ int group_begin(const GnP &p, int g) { return p.table ? p.begin[g] : g * (p.C / p.G); }
+__device__ __forceinline__ int group_begin(const GnP &p, int g) { return p.table ? p.begin[g] : g * p.cg; }
 
 // ---- pairs of fp32 values in one 64-bit register: one instruction adds or multiplies both
 struct f2 { unsigned long long v; };
@@ -138,15 +139,20 @@ __device__ __forceinline__ uint32_t bf16_floor(float v)
 // ReLU without a residual: z = s*(x - mean) + beta > 0, s = gamma*rstd, for bf16 x, as sg ^ x > th. For s > 0 that is x > mean - beta/s, for
 // s < 0 -x > -(mean - beta/s), for s = 0 a constant. What fp32 leaves uncertain of the limit hardly ever lies about a bf16 value, and then
 // 64 bits decide.
+__device__ __noinline__ uint32_t relu_limit_exact(float mean, float rstd, float gamma, float beta)         // th, and sg above it
+{
+    const double sd = (double)gamma * (double)rstd, ld = (double)mean - (double)beta / sd;
+    return bf16_floor(__double2float_rd(sd == 0.0 ? (beta > 0.f ? -INFINITY : INFINITY) : sd < 0.0 ? -ld : ld)) | (sd < 0.0 ? 0x80000000u : 0u);
+}
 __device__ __forceinline__ void relu_limit(float mean, float rstd, float gamma, float beta, uint32_t &th, uint32_t &sg)
 {
-    const float s = gamma * rstd, q = beta / s, lim = s < 0.f ? q - mean : mean - q, off = 5e-7f * (fabsf(mean) + fabsf(q));
+    const float s = gamma * rstd, q = __fdividef(beta, s), lim = s < 0.f ? q - mean : mean - q, off = 1e-6f * (fabsf(mean) + fabsf(q));
     sg = s < 0.f ? 0x8000u : 0u;
     th = bf16_floor(lim - off);
-    if (th != bf16_floor(lim + off) || !(fabsf(lim) < 1e30f) || !(fabsf(s) > 1e-30f)) {
-        const double sd = (double)gamma * (double)rstd, ld = (double)mean - (double)beta / sd;
-        sg = sd < 0.0 ? 0x8000u : 0u;
-        th = bf16_floor(__double2float_rd(sd == 0.0 ? (beta > 0.f ? -INFINITY : INFINITY) : sd < 0.0 ? -ld : ld));
+    if (th != bf16_floor(lim + off) || !(fabsf(lim) < 1e30f) || !(fabsf(s) > 1e-30f && fabsf(s) < 1e30f)) {
+        th = relu_limit_exact(mean, rstd, gamma, beta);
+        sg = th >> 16;
+        th &= 0xffffu;
     }
 }
 
@@ -232,10 +238,9 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         Pos at;                                                          // of batch 0
     };
     const auto moved = [&](const Pos &o, int b) { return Pos{o.v + (uint32_t)b * step_v, o.q + (uint32_t)b * step_q, o.s + (uint32_t)b * step_s}; };
-    const int units = p.N * p.slabs;
-    const auto source = [&](int unit) {
+    const auto source = [&](int n, int sl) {
         Src g{};
-        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0;
+        const int v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0;
         const size_t pix = (size_t)n * p.HW + first;
         const int cv = pr0 < p.ppb && cv0 < nv ? cv0 : 0, cq = (v0 + cv) * 8 < p.C ? cv : 0;
         if (PACKED) {
@@ -273,14 +278,15 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     // (these loads first: behind the ring's copies they would wait for those)
     const bool ahead = BWD && p.gs <= p.threads;                         // a unit's statistics are fetched before they are needed
     float next_mean = 0.f, next_rstd = 0.f;
-    const auto fetch_stats = [&](int unit) {
-        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, g = p.slab_g[sl] + t;
+    const auto fetch_stats = [&](int n, int sl) {
+        const int g = p.slab_g[sl] + t;
         if (ahead && g < p.slab_g[sl + 1]) {
             next_mean = a.mean[(size_t)n * p.G + g];
             next_rstd = a.rstd[(size_t)n * p.G + g];
         }
     };
-    fetch_stats(cluster);
+    int n = p.slabs == 1 ? cluster : cluster / p.slabs, sl = cluster - n * p.slabs;      // the unit: image and slab
+    fetch_stats(n, sl);
     // (A pad lane's z must not be near 0, see gradient: its beta is 1.) Every load comes before the ring's copies, behind which it would wait
     // for them all (10 us where the device has started everywhere at once); the first is stored behind them, its latency is theirs.
     const float gam0 = t < p.C ? a.gamma[t] : 0.f, bet0 = t < p.C ? a.beta[t] : 1.f;
@@ -288,7 +294,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         gam[c] = c < p.C ? a.gamma[c] : 0.f;
         bet[c] = c < p.C ? a.beta[c] : 1.f;
     }
-    Src src = source(cluster);
+    Src src = source(n, sl);
     __syncthreads();                                                     // (every warp's loads are on their way)
     // (as much as keeps the memory busy until the first unit's constants are there; more would hold its threads up at the first barrier, copies being
     // accepted at the rate at which the memory serves them)
@@ -305,14 +311,16 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     const float inv_hw = 1.f / (float)p.HW;
     const int whole = p.HW / p.share;                                    // blocks with all their pixels
     const float rest = (float)(p.HW - whole * p.share);                  // pixels of the one behind them
-    for (int unit = cluster; unit < units; unit += p.clusters, dir ^= 1, ++it) {
-        const int n = p.slabs == 1 ? unit : unit / p.slabs, sl = unit - n * p.slabs, v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0, gb = p.slab_g[sl], ge = p.slab_g[sl + 1];
+    while (n < p.N) {
+        int next_n = n + p.step_n, next_s = sl + p.step_s;
+        if (next_s >= p.slabs) { next_s -= p.slabs; next_n += 1; }
+        const bool more = next_n < p.N;
+        const int v0 = p.slab_v[sl], nv = p.slab_v[sl + 1] - v0, gb = p.slab_g[sl], ge = p.slab_g[sl + 1];
         const bool lane_ok = pr0 < p.ppb && cv0 < nv;
         const int cv = v0 + (lane_ok ? cv0 : 0), c0 = cv * 8;           // the thread's vector and its first channel
         const bool has = c0 < p.C;                                       // it holds channels, not pad lanes only
         const uint4 keep = act8::keep_bits(c0, p.C);
         const size_t base = (size_t)n * p.HW + first;                    // the block's first pixel
-        const bool more = unit + p.clusters < units;
         // (so that a batch of the first walk always has B - 1 groups behind it when it is waited for)
         if (it > 0)
             for (int b = NB; b < B; ++b) copy_commit();
@@ -330,16 +338,16 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             else copy_wait<B - 1>();
             __syncthreads();
             // the average over the group's channels of the block's first pixels: as near the mean as a few values tell
-            const int rows = min(min(4, p.ppb), mine), per = 32 / p.gl, l = lane & (p.gl - 1);
+            const int rows = min(min(4, p.ppb), mine), gl = 1 << p.gl, per = 32 >> p.gl, l = lane & (gl - 1);
             const uint8_t *px = smem + p.sm_ring + (dir ? (B - 1) * U * kRowX : 0u);
             for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
-                const int g = g0 + lane / p.gl;
+                const int g = g0 + (lane >> p.gl);
                 const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
                 float v = 0.f;
-                for (int c = b + l; c < e; c += p.gl)
+                for (int c = b + l; c < e; c += gl)
                     for (int r = 0; r < rows; ++r)
                         v += __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(px + (size_t)(r * p.rl + (c >> 3) - v0) * 16 + (c & 7) * 2));
-                for (int o = p.gl >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+                for (int o = gl >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
                 if (l == 0 && g < ge) grp[g] = rows > 0 ? v / (float)(rows * (e - b)) : 0.f;
             }
         }
@@ -504,7 +512,9 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         const uint4 keep_own = lane_ok ? keep : make_uint4(0u, 0u, 0u, 0u);
         uint32_t s = s_first;
         Pos here = src.at, then = moved(src.at, B);
-        for (int b = 0; b < NB; ++b) {
+        int b = 0;
+        do {
+          for (const int end = min(b + 64 / U, NB); b < end; ++b) {
             copy_wait<B - 1>();
             const bool all = b < full;
             if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
@@ -563,21 +573,21 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             copy_commit();
             then = moved(then, 1);
             here = moved(here, 1);
-            if ((b & (64 / U - 1)) == 64 / U - 1 || b == NB - 1) flush();
             s = s == s_last ? s_first : s + s_step;
-        }
-        if (NB == 0) flush();
+          }
+          flush();
+        } while (b < NB);
         // ---- a group's sums over the threads' rows and its channels
         __syncthreads();
         if (p.cl > 1 && it == 0) cluster_wait();
         {
             // a group's lanes: gc of them take its channels, the others more of the threads' rows
-            const int per = 32 / p.gl, l = lane & (p.gl - 1), lc = l & (p.gc - 1), lr = l / p.gc, nr = p.gl / p.gc, buf = it & 1;
+            const int gl = 1 << p.gl, gc = 1 << p.gc, per = 32 >> p.gl, l = lane & (gl - 1), lc = l & (gc - 1), lr = l >> p.gc, nr = gl >> p.gc, buf = it & 1;
             for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
-                const int g = g0 + lane / p.gl;
+                const int g = g0 + (lane >> p.gl);
                 const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
                 float f0 = 0.f, f1 = 0.f;
-                for (int c = b + lc; c < e; c += p.gc) {
+                for (int c = b + lc; c < e; c += gc) {
                     const float *src = red + (lr * p.rl + (c >> 3) - v0) * 17 + (c & 7);
                     float w0 = 0.f, w1 = 0.f;
 #pragma unroll 4
@@ -586,7 +596,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     f0 = fmaf(f, w0, f0);
                     f1 = fmaf(f, w1, f1);
                 }
-                for (int o = p.gl >> 1; o; o >>= 1) {
+                for (int o = gl >> 1; o; o >>= 1) {
                     f0 += __shfl_xor_sync(0xffffffffu, f0, o);
                     f1 += __shfl_xor_sync(0xffffffffu, f1, o);
                 }
@@ -596,7 +606,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     f0 = g < ge && mine > 0 ? grp[g] + d : 0.f;
                 }
                 if (g < ge)
-                    for (int r = l; r < p.cl; r += p.gl) {
+                    for (int r = l; r < p.cl; r += gl) {
                         float2 *to = xch + (buf * p.cl + rank) * p.gs + (g - gb);
                         if (p.cl == 1) *to = make_float2(f0, f1);
                         else st_cluster_2f(sm100::map_to_rank(sm100::smem_u32(to), (uint32_t)r), f0, f1);
@@ -665,7 +675,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 if (BWD) be[i] = fma2(nm[i], kz[i], be[i]);
             }
         }
-        if (more) fetch_stats(unit + p.clusters);
+        if (more) fetch_stats(next_n, next_s);
         // ---- second walk, backwards: the results
         const bool want_y = !BWD || (PACKED && a.y);
         // the unit's first pixel in dx, dresidual and y
@@ -740,7 +750,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 bring(src, moved(here, -B), s, true);
             } else if (more) {
                 const int m = kept - 1 - b;
-                if (m == 0) src = source(unit + p.clusters);
+                if (m == 0) src = source(next_n, next_s);
                 bring(src, moved(src.at, m), (uint32_t)(dir ? m : B - 1 - m) * kPlace, m < full);
             }
             copy_commit();
@@ -759,6 +769,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 acc[c] += w0 + u0;
                 acc[p.ld + c] += (w1 + u1) * grp[p.G + gid[c]];
             }
+        n = next_n; sl = next_s; dir ^= 1; ++it;
     }
     // ---- the block's row of sums
     if (BWD) {
@@ -843,7 +854,7 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     if (p->table)
         for (int g = 0; g <= d->groups; ++g) p->begin[g] = (uint16_t)b[g];
     p->N = d->N; p->HW = (int)hw; p->C = d->C; p->ld = d->ld; p->LV = d->ld / 8; p->ldq = d->ldq; p->nb = pt_ceil_div(d->C, act8::kBlock);
-    p->G = d->groups; p->eps = d->eps;
+    p->G = d->groups; p->cg = d->C / d->groups; p->eps = d->eps;
     p->w = p->LV >= 3 ? 4 : p->LV;
     return PT_OK;
 }
@@ -888,10 +899,9 @@ size_t gn_shape(GnP *p, int mode, bool res, int cl)
     // lanes of a group: as many as there are for it; as many of them for its channels as it has
     int most = 1;
     for (int g = 0; g < p->G; g += p->table ? 1 : p->G) most = most > gn_begin(*p, g + 1) - gn_begin(*p, g) ? most : gn_begin(*p, g + 1) - gn_begin(*p, g);
-    p->gl = 1;
-    while (p->gl < 32 && 2 * p->gl * p->gs <= p->threads && p->gl < most * p->ppb) p->gl *= 2;
-    p->gc = 1;
-    while (p->gc < p->gl && p->gc < most) p->gc *= 2;
+    p->gl = p->gc = 0;
+    while (p->gl < 5 && (2 << p->gl) * p->gs <= p->threads && (1 << p->gl) < most * p->ppb) p->gl += 1;
+    while (p->gc < p->gl && (1 << p->gc) < most) p->gc += 1;
     size_t at = 0;
     const auto part = [&](unsigned *off, size_t bytes) { *off = (unsigned)at; at += pt_align_up(bytes, 16); };
     part(&p->sm_ring, (size_t)kGnThreads * gn_ring(mode, res));
@@ -972,6 +982,7 @@ pt_status gn_plan(pt_ctx *c, GnKernel kernel, int index, int mode, bool res, GnP
             const int most = (smem <= kGnSmem ? kGnBlocks : 1) * c->sm_count / cl, units = q.N * q.slabs;
             n = n < most ? n : most;
             r.clusters = n < units ? n : units;
+            r.step_n = r.clusters / r.slabs; r.step_s = r.clusters % r.slabs;
             const bool shared = r.clusters * cl > c->sm_count;
             const double rows = (double)pt_ceil_div(r.share, r.ppb) * r.threads / kGnThreads, narrow = q.rl < 4 && q.slabs > 1 ? 1.25 : 1.0;
             const double us = pt_ceil_div(units, r.clusters) * (4.5 + rows * row * narrow * (shared ? 1.8 : 1.0)) + (cl > 1 ? 0.7 : 0.0) + (shared ? 1.0 : 0.0);
