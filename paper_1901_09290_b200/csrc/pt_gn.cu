@@ -90,16 +90,23 @@ __device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32
 // SiLU works on w = -z * log2(e), which costs nothing: the factor is in the constants that give z. sigmoid(z) = 1/(1 + 2^w), 2 ulp and
 // |z| * 2^-24 off. One reciprocal serves a pair, 1/a = b/(a*b): the special-function units take 8 cycles for an instruction of a warp, and
 // with two exponentials and two reciprocals per pair, twice in the backward pass, they were the bound at 64x56x56x256 (46 us of their time
-// alone; 35 with one reciprocal). 2^w stops at 2^60, a sigmoid of 1e-18, so that a*b is finite. (A NaN does not come through: the
-// result is only ever multiplied by w.)
+// alone; 35 with one reciprocal). 2^w stops at 2^60, so that a*b is finite: below z = -41.6 the sigmoid stays 1e-18, and z*sigmoid(z) is
+// 1e-9 at most where |z| < 2^30. A residual, which may be of the type's lowest value, is taken as -2^20 at least (a clamp of w itself took
+// 12 % longer). A NaN stays in w and leaves its neighbour in the pair alone.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ f2 sigmoid_w(f2 w)
 {
     float a, b;
     un2(w, a, b);
-    un2(add2(mk2(ex2(fminf(a, 60.f)), ex2(fminf(b, 60.f))), mk2(1.f, 1.f)), a, b);
+    un2(add2(mk2(fminf(ex2(a), 1.152921504606846976e18f), fminf(ex2(b), 1.152921504606846976e18f)), mk2(1.f, 1.f)), a, b);
     const float r = rcp(a * b);
     return mk2(r * b, r * a);
+}
+__device__ __forceinline__ f2 silu_residual(uint32_t w)
+{
+    const uint32_t low = 0xc980c980u;                                    // -2^20, twice
+    const __nv_bfloat162 h = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162 *>(&w), *reinterpret_cast<const __nv_bfloat162 *>(&low));
+    return from_bf(*reinterpret_cast<const uint32_t *>(&h));
 }
 
 template <int ACT>
@@ -226,8 +233,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     sm100::grid_dependency_wait();
     sm100::grid_launch_dependents();
     // Offsets in bytes from an image's first pixel of this block: 32 bits, added to addresses that all threads share.
-    const uint32_t row = (uint32_t)p.ld * 2u, step_v = (uint32_t)step * row, step_q = (uint32_t)(step * p.ldq), step_s = (uint32_t)(step * p.nb);
-    const uint32_t row_u = (uint32_t)p.ppb * row, row_q = (uint32_t)(p.ppb * p.ldq), row_s = (uint32_t)(p.ppb * p.nb);   // from one of a thread's pixels to the next
+    const uint32_t row = (uint32_t)p.ld * 2u, step_v = (uint32_t)step * row, step_q = (uint32_t)step * (uint32_t)p.ldq, step_s = (uint32_t)step * (uint32_t)p.nb;
+    const uint32_t row_u = (uint32_t)p.ppb * row, row_q = (uint32_t)p.ppb * (uint32_t)p.ldq, row_s = (uint32_t)p.ppb * (uint32_t)p.nb;   // from one of a thread's pixels to the next
     const auto bytes = [](const void *q) { return reinterpret_cast<const uint8_t *>(q); };
     // A unit's tensors from the block's first pixel and the slab's first channel on, and the thread's vector there. Threads without a vector
     // of their own (t >= rl * ppb, lanes behind a narrower slab or that fill up a checkpoint's block) read vector 0 and store nothing. Vectors
@@ -245,7 +252,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         const int cv = pr0 < p.ppb && cv0 < nv ? cv0 : 0, cq = (v0 + cv) * 8 < p.C ? cv : 0;
         if (PACKED) {
             g.q = a.codes_in + pix * p.ldq + v0 * 8; g.s = a.scales_in + pix * p.nb + (v0 >> 2);
-            g.at.q = (uint32_t)(pr * p.ldq) + (uint32_t)cq * 8u; g.at.s = (uint32_t)(pr * p.nb) + ((uint32_t)cq >> 2);
+            g.at.q = (uint32_t)pr * (uint32_t)p.ldq + (uint32_t)cq * 8u; g.at.s = (uint32_t)pr * (uint32_t)p.nb + ((uint32_t)cq >> 2);
         } else {
             g.x = bytes(a.x) + pix * row + v0 * 16;
         }
@@ -366,7 +373,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 if (BWD) {
                     kk[j] = gam[c] * grp[p.G + g];
                     b[j] = bet[c];
-                    be_max = fmaxf(be_max, 1e-6f * fmaxf(fabsf(b[j]), fabsf(fmaf(m[j], kk[j], b[j]))));
+                    be_max = fmaxf(be_max, 1e-6f * fabsf(b[j]));
                     if (ACT == PT_ACT_SILU) b[j] *= -kLog2e;
                 }
                 if (BWD && ACT == PT_ACT_RELU && !RES) {
@@ -406,8 +413,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 x[0] = from_bf(w.x.x); x[1] = from_bf(w.x.y); x[2] = from_bf(w.x.z); x[3] = from_bf(w.x.w);
             }
         };
-        // dz: in place of dy's words where it is dy's bits under a mask, and as pairs. d: what k and be are about, x - mean in the first
-        // walk, x in the second.
+        // dz: in place of dy's words where it is dy's bits under a mask, and as pairs. d: x - mean.
         const auto gradient = [&](Raw &w, const f2 (&d)[4], f2 (&z)[4], f2 (&dz)[4], bool want_z) {
             uint32_t *g = reinterpret_cast<uint32_t *>(&w.dy);
             const uint32_t *xb = reinterpret_cast<const uint32_t *>(&w.x), *rb = reinterpret_cast<const uint32_t *>(&w.res);
@@ -415,7 +421,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     z[i] = fma2(d[i], kz[i], be[i]);
-                    if (RES) z[i] = ACT == PT_ACT_SILU ? fma2(from_bf(rb[i]), mk2(-kLog2e, -kLog2e), z[i]) : add2(z[i], from_bf(rb[i]));
+                    if (RES) z[i] = ACT == PT_ACT_SILU ? fma2(silu_residual(rb[i]), mk2(-kLog2e, -kLog2e), z[i]) : add2(z[i], from_bf(rb[i]));
                 }
             if (ACT == PT_ACT_RELU && !RES) {
 #pragma unroll
@@ -425,9 +431,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 }
             }
             if (ACT == PT_ACT_RELU && RES) {
-                // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |residual| + |beta| + |beta - mean*k| (the
-                // second walk's constant): there 64 bits decide. One test for the
-                // eight values, the least |z| against the largest |residual|: it is passed a few times in a hundred thousand.
+                // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |residual| + |beta|: there 64 bits decide. One test for the eight
+                // values, the least |z| against the largest |residual| and |beta|: it is passed a few times in a hundred thousand.
                 float zz[8], low = INFINITY;
                 uint32_t top = 0u;
 #pragma unroll
@@ -521,8 +526,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 uint8_t *gq = a.codes + base * p.ldq + (size_t)b * step_q, *gs = a.scales + base * p.nb + (size_t)b * step_s;
                 const auto store = [&](const Raw &w, uint32_t byte, int u) {
                     if (lane_ok && has) {
-                        *reinterpret_cast<uint2 *>(gq + (uint32_t)(pr * p.ldq + c0 + u * (int)row_q)) = act8::encode8(w.x, byte);
-                        if ((cv & 3) == 0) gs[(uint32_t)(pr * p.nb + (cv >> 2) + u * (int)row_s)] = (uint8_t)byte;
+                        *reinterpret_cast<uint2 *>(gq + ((uint32_t)pr * (uint32_t)p.ldq + (uint32_t)c0 + (uint32_t)u * row_q)) = act8::encode8(w.x, byte);
+                        if ((cv & 3) == 0) gs[(uint32_t)pr * (uint32_t)p.nb + (uint32_t)(cv >> 2) + (uint32_t)u * row_s] = (uint8_t)byte;
                     }
                 };
                 if (all) {
@@ -626,7 +631,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     float e0 = 0.f, e1 = 0.f;
                     for (int r = 0; r < p.cl; ++r) { e0 += v[r * p.gs].x; e1 += v[r * p.gs].y; }
                     const float rs = grp[p.G + g], t1 = -(rs * rs * rs * e1 * im);
-                    out[g] = fmaf(-t1, grp[g], -(rs * e0 * im));
+                    out[g] = -(rs * e0 * im);
                     out[p.G + g] = t1;
                 } else {
                     // All blocks but the last have `share` pixels (those behind the last have none). Means are averaged as differences from the
@@ -650,29 +655,28 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             }
         }
         __syncthreads();
-        // The second walk's constants, about x itself: forward, z = x*c1 + c2; backward, z = x*kz + be and the group's terms of dx,
-        // x*c2 + c1. (What x - mean would keep of the last bits is lost in the rounding to bf16: with a mean of r standard deviations z is off by
-        // r * 2^-23, and bf16 values of one mean and 2^-8 of it apart have r < 2^8 or so.)
+        // The second walk's constants: forward, minus the mean, gamma*rstd and beta; backward, the group's terms of dx. (About x - mean: folded
+        // into z = x*k + (beta - mean*k) they would save an addition, and lose z where the variance is far below the mean's square: of a
+        // constant group of 1000, with rstd = 316 from eps, 0.02.)
         f2 c1[4], c2[4];
         {
-            float u[8], v[8];
+            float u[8], v[8], m[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = c0 + j, g = gid[c];
                 u[j] = out[g];
                 v[j] = out[p.G + g];
                 if (!BWD) {
-                    const float mean = v[j];
-                    u[j] *= gam[c];
-                    v[j] = fmaf(-mean, u[j], bet[c]);
-                    if (ACT == PT_ACT_SILU) { u[j] *= -kLog2e; v[j] *= -kLog2e; }
+                    m[j] = -v[j];
+                    u[j] *= ACT == PT_ACT_SILU ? -kLog2e * gam[c] : gam[c];
+                    v[j] = ACT == PT_ACT_SILU ? -kLog2e * bet[c] : bet[c];
                 }
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 c1[i] = mk2(u[2 * i], u[2 * i + 1]);
                 c2[i] = mk2(v[2 * i], v[2 * i + 1]);
-                if (BWD) be[i] = fma2(nm[i], kz[i], be[i]);
+                if (!BWD) nm[i] = mk2(m[2 * i], m[2 * i + 1]);
             }
         }
         if (more) fetch_stats(next_n, next_s);
@@ -686,12 +690,14 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             uint4 o;
             uint32_t *ow = reinterpret_cast<uint32_t *>(&o);
             values(w, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = add2(x[i], nm[i]);
             if (!BWD) {
                 const uint32_t *rb = reinterpret_cast<const uint32_t *>(&w.res);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     f2 y = fma2(x[i], c1[i], c2[i]);
-                    if (RES) y = ACT == PT_ACT_SILU ? fma2(from_bf(rb[i]), mk2(-kLog2e, -kLog2e), y) : add2(y, from_bf(rb[i]));
+                    if (RES) y = ACT == PT_ACT_SILU ? fma2(silu_residual(rb[i]), mk2(-kLog2e, -kLog2e), y) : add2(y, from_bf(rb[i]));
                     ow[i] = to_bf(activate2<ACT>(y));
                 }
                 if (lane_ok) *reinterpret_cast<uint4 *>(gy + at) = act8::and4(o, keep);

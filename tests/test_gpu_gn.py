@@ -250,6 +250,71 @@ def test_infinities_and_nan_stay_in_their_group():
     assert torch.isnan(outs[1][2][:10]).all() and torch.equal(outs[1][2][10:30], outs[0][2][10:30])
 
 
+@pytest.mark.parametrize("act", [1, 2])
+def test_residuals_of_the_lowest_value_and_nan(act):
+    """A residual of the type's lowest value leaves nothing of its element, forward and backward; a NaN in the residual stays in its element.
+    "Nothing" of a SiLU is |z| * sigmoid(z) at the least values the kernel takes for them, 2^20 and 2^-60: 2^-40, a per cent more for what
+    x adds to z (below 10 of 2^20) and the rounding to bf16; times |dy| for the gradient."""
+    nothing = 1.01 * 2.0 ** -40
+    c = Hh.ctx()
+    N, H, C, G = 2, 5, 24, 3
+    x, res, dy, g, b = _inputs(N, H, H, C, 9, True)
+    low = torch.finfo(torch.bfloat16).min
+    hit = torch.zeros((N, H, H, C), dtype=torch.bool)
+    hit[0, 1, 2, 3:12], hit[1, 4, 4, 23], hit[1, 0, 0, 0] = True, True, True
+    res[hit] = low
+    d = B.make_gn_desc(N, H, H, C, G, act=act)
+    gd, bd = g.cuda(), b.cuda()
+    mean, rstd = (torch.empty((N, G), device="cuda") for _ in range(2))
+    y = _out(N, H, H, C, C)
+    xd = x.bfloat16().cuda()
+    B.pt_gn_act_fwd(c, d, xd, res.bfloat16().cuda(), gd, bd, mean, rstd, y)
+    assert float(y.cpu()[hit].abs().max()) <= nothing
+    dx, dres = _out(N, H, H, C, C), _out(N, H, H, C, C)
+    dg, db = (torch.empty(C, device="cuda") for _ in range(2))
+    B.pt_gn_act_bwd(c, d, xd, res.bfloat16().cuda(), dy.bfloat16().cuda(), gd, bd, mean, rstd, dx, dres, dg, db, _ws(c, d))
+    m, s = mean.cpu().numpy(), rstd.cpu().numpy()
+    rdx, rdz, rdg, rdb, _ = oracle.gn_act_bwd(x.numpy(), dy.numpy(), g.numpy(), b.numpy(), m, s, oracle.group_begin(C, G), res.numpy(), act)
+    assert bool((dres.cpu()[hit].abs() <= nothing * dy[hit].abs()).all()) and torch.isfinite(dx).all()
+    ady = np.abs(dy.double().numpy())
+    _close(_take(dres, C), rdz, 1e-5 * ady, "dresidual")
+    _close(db.cpu().numpy(), rdb, 1e-5 * ady.sum((0, 1, 2)), "dbeta", bf16=False)
+    # |dx| is rstd * a few |dy| here: all of its terms are below 40
+    _close(_take(dx, C), rdx, 1e-5 * 40 * s.max() * np.ones_like(rdx), "dx")
+    # a NaN
+    clean, y2 = res.clone(), _out(N, H, H, C, C)
+    res[0, 2, 2, 5] = float("nan")
+    B.pt_gn_act_fwd(c, d, xd, res.bfloat16().cuda(), gd, bd, mean, rstd, y2)
+    bad = torch.isnan(y2.cpu())
+    assert bad[0, 2, 2, 5] and int(bad.sum()) == 1 and torch.equal(y2.cpu()[~bad], y.cpu()[~bad]) and not torch.isnan(clean).any()
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+def test_groups_without_variance(act):
+    """A group of equal values far from 0 is its beta: x - mean is 0, however large 1/sqrt(eps) is. (The fp32 mean of equal bf16 values is exact.)"""
+    c = Hh.ctx()
+    N, H, C, G = 2, 6, 16, 2
+    x = torch.full((N, H, H, C), 1000.0)
+    x[..., 8:] = -0.0078125
+    _, res, dy, g, b = _inputs(N, H, H, C, 10, True)
+    d = B.make_gn_desc(N, H, H, C, G, act=act)
+    mean, rstd = (torch.empty((N, G), device="cuda") for _ in range(2))
+    for r in (None, res):
+        y = _out(N, H, H, C, C)
+        B.pt_gn_act_fwd(c, d, x.bfloat16().cuda(), None if r is None else r.bfloat16().cuda(), g.cuda(), b.cuda(), mean, rstd, y)
+        z = b.double().numpy() + (0.0 if r is None else r.double().numpy()) + np.zeros((N, H, H, C))
+        _close(_take(y, C), oracle._act(z, act), 1e-5 * (np.abs(z) + 1), "y")
+    assert torch.equal(mean.cpu(), torch.tensor([[1000.0, -0.0078125]] * N))
+    # the gradients at such values, against the formula's
+    dx, dg, db = _out(N, H, H, C, C), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    B.pt_gn_act_bwd(c, d, x.bfloat16().cuda(), None, dy.bfloat16().cuda(), g.cuda(), b.cuda(), mean, rstd, dx, None, dg, db, _ws(c, d))
+    s = rstd.cpu().numpy()
+    rdx, _, rdg, rdb, _ = oracle.gn_act_bwd(x.numpy(), dy.numpy(), g.numpy(), b.numpy(), mean.cpu().numpy(), s, oracle.group_begin(C, G), None, act)
+    _close(_take(dx, C), rdx, 1e-5 * 10 * s.max() * np.ones_like(rdx), "dx")      # (terms: |gamma * dy| < 8 and its mean, times rstd)
+    _close(db.cpu().numpy(), rdb, 1e-5 * np.abs(dy.numpy()).sum((0, 1, 2)), "dbeta", bf16=False)
+    assert float(dg.abs().max()) == 0.0
+
+
 def test_relu_is_decided_exactly_at_zero():
     """Values whose z is 0 or the smallest step beside it: gradients pass where z > 0 in exact arithmetic."""
     c = Hh.ctx()
