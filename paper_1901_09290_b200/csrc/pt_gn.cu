@@ -443,14 +443,14 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 // Where z is near 0, fp32 leaves it wrong by less than 2^-22 of |residual| + |beta|: there 64 bits decide. One test for the eight
                 // values, the least |z| against the largest |residual| and |beta|: it is passed a few times in a hundred thousand.
                 float zz[8], low = INFINITY;
-                uint32_t top = 0u;
+                __nv_bfloat162 top = __float2bfloat162_rn(0.f);          // (a NaN, in a pad lane too, leaves the others' maximum alone)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     un2(z[i], zz[2 * i], zz[2 * i + 1]);
                     low = fminf(low, fminf(fabsf(zz[2 * i]), fabsf(zz[2 * i + 1])));
-                    top = __vmaxu2(top, rb[i] & 0x7fff7fffu);
+                    top = __hmax2(top, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&rb[i])));
                 }
-                const float rmax = fmaxf(__uint_as_float(top << 16), __uint_as_float(top & 0xffff0000u));
+                const float rmax = fmaxf(__low2float(top), __high2float(top));
                 if (low <= fmaf(rmax, 1e-6f, be_max)) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {

@@ -336,6 +336,77 @@ def test_relu_is_decided_exactly_at_zero():
             assert torch.equal(db.cpu().double(), want) and torch.equal(dres.cpu() > 0, z > 0)
 
 
+@pytest.mark.parametrize("nan_at", [(0,), (1,), (0, 1), (6, 7)])
+def test_relu_is_decided_exactly_beside_a_nan(nan_at):
+    """A NaN in the residual, or in its pad lanes, which are never used, leaves the decisions of the other values alone. gamma * rstd =
+    0.75 * fl(2/3) = 0.5 + 2^-26, which fp32 rounds to 0.5, so that z = 256 * gamma * rstd - 128 = 2^-18 is 0 in fp32 and positive."""
+    c = Hh.ctx()
+    N, H, C, ld = 1, 8, 6, 8
+    x, r = torch.full((N, H, H, ld), 256.0), torch.full((N, H, H, ld), -128.0)
+    r[..., list(nan_at)] = float("nan")
+    mean, rstd = torch.zeros((1, 1), device="cuda"), torch.full((1, 1), 2.0 / 3.0, device="cuda")
+    g, b = torch.full((C,), 0.75, device="cuda"), torch.zeros(C, device="cuda")
+    d = B.make_gn_desc(N, H, H, C, 1, ld, act=B.PT_ACT_RELU)
+    dy, dx, dres = torch.ones((N, H, H, ld), dtype=torch.bfloat16, device="cuda"), _out(N, H, H, C, ld), _out(N, H, H, C, ld)
+    dg, db = (torch.empty(C, device="cuda") for _ in range(2))
+    B.pt_gn_act_bwd(c, d, x.bfloat16().cuda(), r.bfloat16().cuda(), dy, g, b, mean, rstd, dx, dres, dg, db, _ws(c, d))
+    want = np.array([0.0 if k in nan_at else 1.0 for k in range(C)])
+    assert np.array_equal(_take(dres, C), np.broadcast_to(want, (N, H, H, C)))
+    assert np.array_equal(db.cpu().numpy(), want * H * H)
+
+
+# units in several rounds over the device's blocks, whose pixels a ring does not hold, and in slabs of channels with ragged groups
+@pytest.mark.parametrize("shape", [(310, 18, 18, 64, 4), (333, 5, 6, 264, 11), (700, 5, 3, 72, 9), (160, 23, 17, 130, 6)])
+def test_many_units_of_a_cluster(shape):
+    check_forward(*shape, 2, True)
+    check_forward(*shape, 1, False)
+    check_backward(*shape, 1, True)
+    check_backward(*shape, 2, False)
+
+
+@pytest.mark.parametrize("shape", [(610, 3, 3, 64, 4), (333, 4, 3, 264, 11), (700, 2, 3, 72, 9), (6, 23, 17, 130, 6)])
+def test_many_units_of_a_cluster_with_checkpoints(shape):
+    check_forward(*shape, 2, True, pack=True)
+    check_backward(*shape, 1, True, packed=True)
+    check_backward(*shape, 2, False, packed=True)
+
+
+def test_graphs_of_their_own_and_an_eager_call_between():
+    """Two captured passes, a workspace each, replayed in turn and at once beside an eager one: the same bits throughout."""
+    c = Hh.ctx()
+    N, H, C, G = 40, 12, 48, 6
+    x, res, dy, g, b = _inputs(N, H, H, C, 11, True)
+    d = B.make_gn_desc(N, H, H, C, G, C, act=B.PT_ACT_RELU)
+    xd, rd, dyd, gd, bd = Hh.to_dev_padded(x, C), Hh.to_dev_padded(res, C), Hh.to_dev_padded(dy, C), g.cuda(), b.cuda()
+    mean, rstd = (torch.zeros((N, G), device="cuda") for _ in range(2))
+    B.pt_gn_act_fwd(c, d, xd, rd, gd, bd, mean, rstd, _out(N, H, H, C, C))
+
+    def bufs():
+        return [_out(N, H, H, C, C), _out(N, H, H, C, C), torch.zeros(C, device="cuda"), torch.zeros(C, device="cuda"), _ws(c, d)]
+
+    go = lambda o, stream=None: B.pt_gn_act_bwd(c, d, xd, rd, dyd, gd, bd, mean, rstd, *o, stream)
+    eager = bufs()
+    go(eager)
+    torch.cuda.synchronize()
+    graphs, outs, sides = [], [bufs(), bufs()], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for o in outs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            go(o)
+        graphs.append(graph)
+    later = bufs()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for graph, side in zip(graphs, sides):
+            with torch.cuda.stream(side):
+                graph.replay()
+        go(later)
+    torch.cuda.synchronize()
+    c.poll()
+    for o in outs + [later]:
+        assert all(torch.equal(p, q) for p, q in zip(eager[:4], o[:4]))
+
+
 def test_identical_runs_streams_and_graphs():
     c = Hh.ctx()
     N, H, C, G = 24, 20, 77, 7
