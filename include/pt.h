@@ -271,7 +271,8 @@ pt_status pt_bn_relu_bwd(pt_ctx *ctx, const pt_bn_desc *d, const void *x, const 
  * An infinity or a NaN in x makes the outputs of its image and group NaN; a NaN in the residual stays in its element of y. PT_ACT_SILU wants
  * |gamma*xhat + beta| below 2^30 and a residual below 2^126 (it may be as low as the type goes, and leaves 0 then).
  * The current device must be the context's. PT_ERR_INVALID_ARG for bad sizes, pitches, alignment, groups, missing pointers or another
- * current device; PT_ERR_UNSUPPORTED for ld > 2048, an image of 4 GB or more, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.
+ * current device; PT_ERR_UNSUPPORTED for ld > 2048, more than 2^24 images, an image of 4 GB or
+ * more, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.
  * ------------------------------------------------------------------------------------------ */
 enum { PT_ACT_NONE = 0, PT_ACT_RELU = 1, PT_ACT_SILU = 2 };
 typedef struct {

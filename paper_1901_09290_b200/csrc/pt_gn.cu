@@ -31,6 +31,7 @@ namespace {
 constexpr int kGnThreads = 256;              // most threads of a block
 constexpr int kGnTable = 256;                // most groups of a table
 constexpr int kGnMaxLd = 2048;
+constexpr int kGnMaxN = 1 << 24;             // most images: units, and steps behind the last one, are counted in 32 bits
 constexpr int kGnMaxCluster = 16;
 constexpr int kGnExchange = 1024;            // most entries (blocks of the cluster x groups) of one exchange buffer
 constexpr int kGnSlabs = 32;                 // most slabs of channels
@@ -863,7 +864,7 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     } else if (d->C % d->groups) {
         return PT_ERR_INVALID_ARG;
     }
-    if (d->ld > kGnMaxLd || (p->table && d->groups > kGnTable)) return PT_ERR_UNSUPPORTED;
+    if (d->N > kGnMaxN || d->ld > kGnMaxLd || (p->table && d->groups > kGnTable)) return PT_ERR_UNSUPPORTED;
     const long long hw = (long long)d->H * d->W;
     if (hw * d->ld * 2 >= 0x100000000ll || (codes && hw * d->ldq >= 0x100000000ll)) return PT_ERR_UNSUPPORTED;    // (offsets in an image have 32 bits)
     if (p->table)

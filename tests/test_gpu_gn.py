@@ -563,3 +563,15 @@ def test_empty_checkpoint_and_refusals():
     refused(lambda: bwd(good, ws=ws[:ws.numel() - 16]), 3)
     with pytest.raises(ValueError):
         gd(groups=3, begin=[0, 32])
+
+
+def test_more_images_than_units_are_counted_in_are_refused():
+    c = Hh.ctx()
+    t, v, s = torch.zeros(64, dtype=torch.bfloat16, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+    for N in ((1 << 24) + 1, 2 ** 31 - 1):
+        d = B.make_gn_desc(N, 1, 1, 8, 1, 8)
+        assert B.pt_gn_workspace_bytes(c, d) == 0
+        with pytest.raises(B.PtError) as e:
+            B.pt_gn_act_fwd(c, d, t, None, v, v, s, s.clone(), t.clone(), None, None)
+        assert e.value.status == 2
+    assert B.pt_gn_workspace_bytes(c, B.make_gn_desc(1 << 24, 1, 1, 8, 1, 8)) > 0
