@@ -140,10 +140,10 @@ int32_t pt_conv_wgrad_ctas(const pt_ctx *ctx, const pt_conv_desc *d, int32_t *wa
 /* Stream order: the three calls below are ordinary stream work. Their kernels are launched with programmatic stream
  * serialization and read the WEIGHTS before waiting for the preceding kernel of the stream; that is invisible to callers
  * because only kernels that release their dependents early (griddepcontrol.launch_dependents before their last store) can be
- * overtaken: of this library's kernels the convolutions, the batch norms and the read-only sweeps and the finish of the lasso step do that, and none of them
- * writes weights (the update of pt_group_lasso_sgd_step and the gather of pt_reconfigure complete before their successors
- * start). A caller's own kernel that writes w and releases its dependents early must be followed by an event or another
- * kernel before a convolution reads w. */
+ * overtaken: of this library's kernels the convolutions, the batch and group norms, the checkpoint passes and the read-only sweeps and the finish of
+ * the lasso step do that, and none of them writes weights (the update of pt_group_lasso_sgd_step and the gather of pt_reconfigure complete before their successors
+ * start; what pt_act_unpack restores counts as an activation). A caller's own kernel that writes w and releases its dependents early must be followed by an event or another
+ * kernel before a convolution reads w, and so must pt_act_unpack into a w. */
 /* y[n,p,q,k] = sum_{r,s,c} x[n, p*stride-pad+r, q*stride-pad+s, c] * w[k,r,s,c], zero outside the image.
  * x: bf16 [N][H][W][ldx]; w: bf16 shadow [K][R][S][ldw]; y: [N][P][Q][ldy] bf16 or fp32. fp32 accumulation. */
 pt_status pt_conv_fwd(pt_ctx *ctx, const pt_conv_desc *d, const void *x, const void *w, void *y,
@@ -308,7 +308,8 @@ size_t pt_act_scale_bytes(int64_t npix, int32_t C);
 pt_status pt_act_pack(pt_ctx *ctx, const pt_pack_desc *d, const void *x, void *codes, void *scales, void *stream);
 pt_status pt_act_unpack(pt_ctx *ctx, const pt_pack_desc *d, const void *codes, const void *scales, void *x, void *stream);
 
-/* Bytes of workspace the two backward calls need for this descriptor (0 if it is invalid). */
+/* Bytes of workspace the two backward calls need for this descriptor (0 if it is invalid or unsupported). ws is 16-byte aligned and
+ * belongs to one call at a time: calls that may run at once (streams, replayed graphs) need one each. */
 size_t pt_gn_workspace_bytes(const pt_ctx *ctx, const pt_gn_desc *d);
 
 /* y = act(gamma*xhat + beta + residual). residual may be NULL. save_mean, save_rstd receive what the backward pass needs. codes and

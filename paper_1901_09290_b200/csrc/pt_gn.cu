@@ -799,7 +799,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 }
 
 // dgamma, dbeta: the blocks' rows. A block owns 32 columns; a warp adds every 32nd row of them, all loads before the first addition, then
-// a column's 32 sums: a fixed order, chains of at most ten.
+// a column's 32 sums: a fixed order, chains of at most ten. (Plain loads: the rows are still being written when this kernel starts, so they
+// are not read-only for all of its life.)
 __global__ void __launch_bounds__(1024) gn_finish_kernel(const float *rows, int n, int C, int ld, float *dgamma, float *dbeta)
 {
     __shared__ float part[32][33];
@@ -812,7 +813,7 @@ __global__ void __launch_bounds__(1024) gn_finish_kernel(const float *rows, int 
     for (int r0 = warp; r0 < n; r0 += 10 * 32) {                         // (296 rows are one round)
         float x[10];
 #pragma unroll
-        for (int i = 0; i < 10; ++i) x[i] = e < 2 * ld && r0 + 32 * i < n ? __ldg(src + (r0 + 32 * i) * pitch) : 0.f;
+        for (int i = 0; i < 10; ++i) x[i] = e < 2 * ld && r0 + 32 * i < n ? src[(r0 + 32 * i) * pitch] : 0.f;
 #pragma unroll
         for (int i = 0; i < 10; ++i) v += x[i];
     }
