@@ -27,7 +27,7 @@ __global__ void __launch_bounds__(kPackThreads, kPackBlocks) pack_kernel(const P
     const bool has = pr < p.rows && cv < p.LV, pad = !PACK && pr < p.rows && cv < p.ld / 8;
     const uint4 keep = act8::keep_bits(cv * 8, p.C), zero = make_uint4(0u, 0u, 0u, 0u);
     const int step = U * p.rows;
-    uint32_t ox[U], oq[U], os[U];                                // (a thread block's pixels at a time: far below 4 GB)
+    uint32_t ox[U], oq[U], os[U];                                // (a thread block's pixels at a time: less than 4 GB, see launch_pack)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t r = (uint32_t)(pr + u * p.rows);
@@ -78,11 +78,14 @@ pt_status launch_pack(pt_ctx *c, PackP p, void *x, void *codes, void *scales, cu
     if (p.npix == 0) return PT_OK;
     p.rl = PACK ? pt_ceil_div(p.LV, p.w) * p.w : p.ld / 8;
     p.rows = kPackThreads / p.rl;
+    // Offsets within a thread block's pixels have 32 bits: where codes lie megabytes apart a block takes fewer pixels, so that rows * ldq is
+    // below 2^32. (Four of them at a time only where that holds for all four. Pitches of bf16 are far below.)
+    if ((long long)p.rows * p.ldq > 0xffffffffll) p.rows = (int)(0xffffffffll / p.ldq);
     // Blocks of a few rounds each, four to a place on an SM: both passes at 64x56x56x256 take 56.5 us with one round of blocks that share
     // everything, 53.8 with four, 57.3 with a block for every four pixels a thread. Small tensors: a pixel at a time, spread over more blocks
     // (128x8x8x41: 3.8 us where four at a time took 4.7).
     const long long most = (long long)c->sm_count * kPackBlocks * 4, one = (p.npix + p.rows - 1) / p.rows;
-    const bool four = one >= most;
+    const bool four = one >= most && 4ll * p.rows * p.ldq <= 0xffffffffll;
     const long long need = four ? (one + 3) / 4 : one;
     PT_CUDA_OK(pt_launch_pdl(four ? pack_kernel<PACK, 4> : pack_kernel<PACK, 1>, dim3((unsigned)(need < most ? need : most)), dim3(kPackThreads), 0, st, p,
                              (uint8_t *)x, (uint8_t *)codes, (uint8_t *)scales));
