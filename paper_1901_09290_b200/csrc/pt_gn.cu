@@ -46,6 +46,8 @@ __host__ __device__ constexpr int gn_slot(int mode, bool res) { return (mode == 
 __host__ __device__ constexpr int gn_rows(int mode) { return gn_bwd(mode) ? 2 : 4; }
 // Batches of a thread's ring: what two blocks to an SM have room for.
 __host__ __device__ constexpr int gn_batches(int mode, bool res) { return 290 / (gn_rows(mode) * gn_slot(mode, res)); }
+// Words of a thread's place for its sums: eight pairs, and in the forward pass eight bf16 and a count besides. Odd, so that 32 places share no bank.
+__host__ __device__ constexpr int gn_red(int mode) { return gn_bwd(mode) ? 17 : 21; }
 __host__ __device__ constexpr int gn_ring(int mode, bool res) { return gn_rows(mode) * gn_batches(mode, res) * gn_slot(mode, res); }
 constexpr int kGnBlocks = 2;                 // blocks of an SM: while one exchanges its sums, the other one moves data
 constexpr size_t kGnSmem = 113 * 1024, kGnSmemMost = 226 * 1024;     // shared memory of a block: two on an SM, one
@@ -93,6 +95,13 @@ __device__ __forceinline__ uint32_t to_bf(f2 x)
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
+__device__ __forceinline__ float bf_half(uint32_t w, int i) { return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+// 1/x to some 46 bits, from fp32's by a Newton step.
+__device__ __forceinline__ double inverse(double x) { const double r = (double)(1.f / (float)x); return r * fma(-x, r, 2.0); }
+
+// A group's sums, by direction: fp32 in the backward pass; the forward pass takes a variance from them, for which they are kept in 64 bits.
+template <bool BWD> struct GnSums { typedef float T; typedef float2 T2; };
+template <> struct GnSums<false> { typedef double T; typedef double2 T2; };
 
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
@@ -133,6 +142,10 @@ __device__ __forceinline__ f2 activate2(f2 z)
 __device__ __forceinline__ void st_cluster_2f(uint32_t addr, float a, float b)
 {
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(a), "f"(b) : "memory");
+}
+__device__ __forceinline__ void st_cluster_2f(uint32_t addr, double a, double b)
+{
+    asm volatile("st.shared::cluster.v2.f64 [%0], {%1, %2};" ::"r"(addr), "d"(a), "d"(b) : "memory");
 }
 // The two halves of sm100::cluster_barrier. (Shared memory of another block may be written once that block has started.)
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -217,17 +230,19 @@ template <int MODE, int ACT, bool RES>
 __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_constant__ GnP p, const GnArgs a)
 {
     constexpr bool BWD = gn_bwd(MODE), PACK = MODE == kGnFwdPack, PACKED = MODE == kGnBwdPacked;
-    constexpr int B = gn_batches(MODE, RES), U = gn_rows(MODE);
+    constexpr int B = gn_batches(MODE, RES), U = gn_rows(MODE), kRed = gn_red(MODE);
+    typedef typename GnSums<BWD>::T Sum;
+    typedef typename GnSums<BWD>::T2 Sum2;
     // the ring's parts, [B][U][threads] each: x or codes, dy, residual, scale words
     constexpr uint32_t kXs = PACKED ? 8 : 16, kRowX = kGnThreads * kXs, kRow = kGnThreads * 16, kRowS = kGnThreads * 4, kPlace = U * kRow;
     constexpr uint32_t kDy = B * U * kRowX, kRes = kDy + (BWD ? B * U * kRow : 0), kSc = kRes + (BWD && RES ? B * U * kRow : 0);
     extern __shared__ __align__(128) uint8_t smem[];
     uint16_t *gid = reinterpret_cast<uint16_t *>(smem + p.sm_gid);       // [ld] group of a channel
     float *gam = reinterpret_cast<float *>(smem + p.sm_gam), *bet = reinterpret_cast<float *>(smem + p.sm_bet);      // [ld]
-    float *grps = reinterpret_cast<float *>(smem + p.sm_grp);            // [2][2][G] of alternating images: mean and rstd (backward), pivot
+    float *grps = reinterpret_cast<float *>(smem + p.sm_grp);            // [2][2][G] of alternating images: mean and rstd (backward)
     float *out = grps + 4 * p.G;                                         // [2][G] rstd and mean (forward), the group's terms of dx (backward)
-    float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][17]
-    float2 *xch = reinterpret_cast<float2 *>(smem + p.sm_xch);           // [2][cl][gs]
+    float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][kRed]
+    Sum2 *xch = reinterpret_cast<Sum2 *>(smem + p.sm_xch);               // [2][cl][gs], of alternating images; one without clusters
     float *acc = reinterpret_cast<float *>(smem + p.sm_acc);             // [2][ld] the block's sums of dz and dz * xhat over its units
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = p.threads >> 5;
     const int rank = (int)(blockIdx.x % p.cl), cluster = (int)(blockIdx.x / p.cl);
@@ -341,7 +356,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         // (so that a batch of the first walk always has B - 1 groups behind it when it is waited for)
         if (it > 0)
             for (int b = NB; b < B; ++b) copy_commit();
-        // ---- what the first walk needs of every group: the statistics (backward), or a value near its mean (forward)
+        // ---- what the first walk needs of every group: the statistics (backward)
         float *grp = grps + (it & 1) * 2 * p.G;
         if (BWD && ahead) {
             if (gb + t < ge) { grp[gb + t] = next_mean; grp[p.G + gb + t] = next_rstd; }
@@ -350,43 +365,34 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 grp[g] = a.mean[(size_t)n * p.G + g];
                 grp[p.G + g] = a.rstd[(size_t)n * p.G + g];
             }
-        } else {
-            if (it == 0) copy_wait<kFirst - 1>();
-            else copy_wait<B - 1>();
-            __syncthreads();
-            // the average over the group's channels of the block's first pixels: as near the mean as a few values tell
-            const int rows = min(min(4, p.ppb), mine), gl = 1 << p.gl, per = 32 >> p.gl, l = lane & (gl - 1);
-            const uint8_t *px = smem + p.sm_ring + (dir ? (B - 1) * U * kRowX : 0u);
-            for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
-                const int g = g0 + (lane >> p.gl);
-                const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
-                float v = 0.f;
-                for (int c = b + l; c < e; c += gl)
-                    for (int r = 0; r < rows; ++r)
-                        v += __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(px + (size_t)(r * p.rl + (c >> 3) - v0) * 16 + (c & 7) * 2));
-                for (int o = gl >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-                if (l == 0 && g < ge) grp[g] = rows > 0 ? v / (float)(rows * (e - b)) : 0.f;
-            }
         }
-        __syncthreads();
-        // the thread's constants: minus the mean (or pivot), and in the backward pass gamma*rstd, beta, and the ReLU's limits as bf16: without
-        // a residual, z > 0 exactly where x ^ sgn > thr
+        if (BWD) __syncthreads();
+        // the thread's constants, backward: minus the mean, gamma*rstd, beta, and the ReLU's limits as bf16: without a residual, z > 0 exactly
+        // where x ^ sgn > thr. Forward: minus the pivots, at first the values of the thread's first pixel.
         f2 nm[4], k[4], kz[4], be[4];                                    // (kz: k, or for SiLU what gives w)
         uint32_t thr[4], sgn[4];
         float be_max = 1e-30f;                                           // (z so small that bf16 might not hold it is decided there too)
-        {
+        int taken = 0;                                                   // pixels that the thread's statistics hold (forward)
+        int extra = 0;                                                   // the thread's pixels of the last, partial batch
+        if (!BWD) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) extra += u * p.ppb < tail;
+            if (it == 0) copy_wait<kFirst - 1>();
+            else copy_wait<B - 1>();
+            uint4 v = make_uint4(0u, 0u, 0u, 0u);
+            if (full + extra > 0) v = *reinterpret_cast<const uint4 *>(mine_v + (dir ? (B - 1) * kPlace : 0u));
+            nm[0] = from_bf(v.x ^ 0x80008000u); nm[1] = from_bf(v.y ^ 0x80008000u); nm[2] = from_bf(v.z ^ 0x80008000u); nm[3] = from_bf(v.w ^ 0x80008000u);
+        } else {
             float m[8], kk[8], b[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = c0 + j, g = gid[c];
                 m[j] = -grp[g];
-                if (BWD) {
-                    kk[j] = gam[c] * grp[p.G + g];
-                    b[j] = bet[c];
-                    be_max = fmaxf(be_max, 1e-6f * fabsf(b[j]));
-                    if (ACT == PT_ACT_SILU) b[j] *= -kLog2e;
-                }
-                if (BWD && ACT == PT_ACT_RELU && !RES) {
+                kk[j] = gam[c] * grp[p.G + g];
+                b[j] = bet[c];
+                be_max = fmaxf(be_max, 1e-6f * fabsf(b[j]));
+                if (ACT == PT_ACT_SILU) b[j] *= -kLog2e;
+                if (ACT == PT_ACT_RELU && !RES) {
                     uint32_t th, sg;
                     relu_limit(grp[g], grp[p.G + g], gam[c], bet[c], th, sg);
                     thr[j >> 1] = j & 1 ? thr[j >> 1] | th << 16 : th;
@@ -396,11 +402,9 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 nm[i] = mk2(m[2 * i], m[2 * i + 1]);
-                if (BWD) {
-                    k[i] = mk2(kk[2 * i], kk[2 * i + 1]);
-                    kz[i] = ACT == PT_ACT_SILU ? mul2(k[i], mk2(-kLog2e, -kLog2e)) : k[i];
-                    be[i] = mk2(b[2 * i], b[2 * i + 1]);
-                }
+                k[i] = mk2(kk[2 * i], kk[2 * i + 1]);
+                kz[i] = ACT == PT_ACT_SILU ? mul2(k[i], mk2(-kLog2e, -kLog2e)) : k[i];
+                be[i] = mk2(b[2 * i], b[2 * i + 1]);
             }
         }
         // pixel u of a batch at the ring's place s; os: the thread's place in the scales
@@ -505,22 +509,69 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 s1[i] = fma2(d, x[i], s1[i]);
             }
         };
-        // a thread's chains of additions stay short: every 64 rows they go to its place in shared memory
+        // A thread's chains of additions stay short. Backward: every 64 rows the sums go to the thread's place in shared memory.
+        // Forward: one-pass sums about a pivot lose a variance that is small beside the square of what the pivot is off by, and a first pixel
+        // may be nothing like the rest (a border, a mask). So the thread keeps, for each channel, its pixels' mean, as a pivot of bf16 plus an
+        // offset of fp32, and the sum of squares about that mean; a run's sums are joined to them, and the next run is taken about the new mean.
+        // The runs end behind 4 and every 16 batches: what an odd first pixel leaves in the pivot falls as the pixels grow in number.
         bool flushed = false;
-        const auto flush = [&]() {
-            float *o = red + t * 17;
+        const auto flush = [&](int batches) {
+            float *o = red + t * kRed;
+            if (!BWD) {
+                const int now = (batches < full ? batches : full) * U + (batches > full ? extra : 0), run = now - taken;
+                if (run > 0) {
+                    const float inv = 1.f / (float)run;
+                    float w = 1.f, w2 = 0.f;
+                    if (taken > 0) { w = (float)run / (float)now; w2 = (float)taken * w; }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float u[4];
-                un2(s0[i], u[0], u[1]);
-                un2(s1[i], u[2], u[3]);
-                o[2 * i] = flushed ? o[2 * i] + u[0] : u[0];
-                o[2 * i + 1] = flushed ? o[2 * i + 1] + u[1] : u[1];
-                o[8 + 2 * i] = flushed ? o[8 + 2 * i] + u[2] : u[2];
-                o[9 + 2 * i] = flushed ? o[9 + 2 * i] + u[3] : u[3];
-                s0[i] = s1[i] = mk2(0.f, 0.f);
+                    for (int i = 0; i < 4; ++i) {
+                        float sum[2], sq[2], off[2];
+                        un2(s0[i], sum[0], sum[1]);
+                        un2(s1[i], sq[0], sq[1]);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int j = 2 * i + h;
+                            const float d = sum[h] * inv;
+                            sq[h] = fmaxf(fmaf(-sum[h], d, sq[h]), 0.f);
+                            off[h] = d;
+                            if (taken > 0) {
+                                const float was = o[j], apart = d - was;
+                                sq[h] = fmaf(apart * apart, w2, sq[h] + o[8 + j]);
+                                off[h] = fmaf(apart, w, was);
+                            }
+                            o[8 + j] = sq[h];
+                        }
+                        if (batches < NB) {                              // the pivot of the next run
+                            float q[2];
+                            un2(nm[i], q[0], q[1]);                      // (minus the last one)
+                            const uint32_t word = to_bf(mk2(off[0] - q[0], off[1] - q[1]));
+                            nm[i] = from_bf(word ^ 0x80008000u);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) off[h] -= bf_half(word, h) + q[h];
+                        }
+                        o[2 * i] = off[0];
+                        o[2 * i + 1] = off[1];
+                    }
+                    taken = now;
+                } else if (now == 0) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) o[j] = 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float u[4];
+                    un2(s0[i], u[0], u[1]);
+                    un2(s1[i], u[2], u[3]);
+                    o[2 * i] = flushed ? o[2 * i] + u[0] : u[0];
+                    o[2 * i + 1] = flushed ? o[2 * i + 1] + u[1] : u[1];
+                    o[8 + 2 * i] = flushed ? o[8 + 2 * i] + u[2] : u[2];
+                    o[9 + 2 * i] = flushed ? o[9 + 2 * i] + u[3] : u[3];
+                }
+                flushed = true;
             }
-            flushed = true;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s0[i] = s1[i] = mk2(0.f, 0.f);
         };
         // the ring's places in the order of the walk, and where they begin and end
         const uint32_t s_first = dir ? (B - 1) * kPlace : 0u, s_last = dir ? 0u : (B - 1) * kPlace, s_step = dir ? 0u - kPlace : kPlace;
@@ -529,7 +580,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         Pos here = src.at, then = moved(src.at, B);
         int b = 0;
         do {
-          for (const int end = min(b + 64 / U, NB); b < end; ++b) {
+          for (const int end = min(BWD ? b + 64 / U : b == 0 ? 4 : (b & ~15) + 16, NB); b < end; ++b) {
             copy_wait<B - 1>();
             const bool all = b < full;
             if (PACK) {                                                  // (whole warps: the lanes of a checkpoint's block exchange)
@@ -590,51 +641,82 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
             here = moved(here, 1);
             s = s == s_last ? s_first : s + s_step;
           }
-          flush();
+          flush(b);
         } while (b < NB);
+        if (!BWD) {                                                      // the pivots, behind offsets and squares, and the number of pixels
+#pragma unroll
+            for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t *>(red)[t * kRed + 16 + i] = to_bf(nm[i]) ^ 0x80008000u;
+            red[t * kRed + 20] = (float)taken;
+        }
         // ---- a group's sums over the threads' rows and its channels
         __syncthreads();
         if (p.cl > 1 && it == 0) cluster_wait();
         {
             // a group's lanes: gc of them take its channels, the others more of the threads' rows
-            const int gl = 1 << p.gl, gc = 1 << p.gc, per = 32 >> p.gl, l = lane & (gl - 1), lc = l & (gc - 1), lr = l >> p.gc, nr = gl >> p.gc, buf = it & 1;
+            const int gl = 1 << p.gl, gc = 1 << p.gc, per = 32 >> p.gl, l = lane & (gl - 1), lc = l & (gc - 1), lr = l >> p.gc, nr = gl >> p.gc, buf = p.cl > 1 ? it & 1 : 0;
             for (int g0 = gb + warp * per; g0 < ge; g0 += warps * per) {
                 const int g = g0 + (lane >> p.gl);
                 const int b = g < ge ? group_begin(p, g) : 0, e = g < ge ? group_begin(p, g + 1) : 0;
-                float f0 = 0.f, f1 = 0.f;
-                for (int c = b + lc; c < e; c += gc) {
-                    const float *src = red + (lr * p.rl + (c >> 3) - v0) * 17 + (c & 7);
-                    float w0 = 0.f, w1 = 0.f;
+                Sum f0 = 0, f1 = 0, one = 0;
+                if (!BWD && g < ge && mine > 0) one = inverse((double)mine * (double)(e - b));
+                float ref = 0.f, ref_off = 0.f;
+                if (BWD) {
+                    for (int c = b + lc; c < e; c += gc) {
+                        const float *src = red + (lr * p.rl + (c >> 3) - v0) * kRed + (c & 7);
+                        float w0 = 0.f, w1 = 0.f;
 #pragma unroll 4
-                    for (int r = lr; r < p.ppb; r += nr, src += nr * p.rl * 17) { w0 += src[0]; w1 += src[8]; }
-                    const float f = BWD ? gam[c] : 1.f;
-                    f0 = fmaf(f, w0, f0);
-                    f1 = fmaf(f, w1, f1);
+                        for (int r = lr; r < p.ppb; r += nr, src += nr * p.rl * kRed) { w0 += src[0]; w1 += src[8]; }
+                        f0 += gam[c] * w0;
+                        f1 += gam[c] * w1;
+                    }
+                } else {
+                    // The threads' means as differences from that of the group's first thread and channel, which may be far from the others:
+                    // sums about it in 64 bits.
+                    const auto pivot = [&](const float *place, int c) { return bf_half(reinterpret_cast<const uint32_t *>(place)[16 + ((c & 7) >> 1)], c); };
+                    if (g < ge) {
+                        const float *first_place = red + ((b >> 3) - v0) * kRed;
+                        ref = pivot(first_place, b);
+                        ref_off = first_place[b & 7];
+                    }
+                    float m2 = 0.f;
+                    for (int c = b + lc; c < e; c += gc) {
+                        const float *src = red + (lr * p.rl + (c >> 3) - v0) * kRed;
+#pragma unroll 4
+                        for (int r = lr; r < p.ppb; r += nr, src += nr * p.rl * kRed) {
+                            const Sum d = (Sum)((pivot(src, c) - ref) + (src[c & 7] - ref_off)), dn = d * (Sum)src[20];
+                            m2 += src[8 + (c & 7)];
+                            f0 += dn;
+                            f1 += dn * d;
+                        }
+                    }
+                    f1 += (Sum)m2;
                 }
                 for (int o = gl >> 1; o; o >>= 1) {
                     f0 += __shfl_xor_sync(0xffffffffu, f0, o);
                     f1 += __shfl_xor_sync(0xffffffffu, f1, o);
                 }
                 if (!BWD) {                                              // the block's mean and sum of squares about it
-                    const float d = mine > 0 ? f0 / ((float)mine * (float)(e - b)) : 0.f;
-                    f1 = fmaxf(f1 - f0 * d, 0.f);
-                    f0 = g < ge && mine > 0 ? grp[g] + d : 0.f;
+                    const Sum d = f0 * one;
+                    f1 -= f0 * d;
+                    f1 = f1 < 0 ? 0 : f1;
+                    f0 = (Sum)ref + (Sum)ref_off + d;
                 }
                 if (g < ge)
                     for (int r = l; r < p.cl; r += gl) {
-                        float2 *to = xch + (buf * p.cl + rank) * p.gs + (g - gb);
-                        if (p.cl == 1) *to = make_float2(f0, f1);
+                        Sum2 *to = xch + (buf * p.cl + rank) * p.gs + (g - gb);
+                        if (p.cl == 1) { to->x = f0; to->y = f1; }
                         else st_cluster_2f(sm100::map_to_rank(sm100::smem_u32(to), (uint32_t)r), f0, f1);
                     }
             }
             // (divided before the wait)
             const int own_g = gb + t;
+            const Sum inv_n = BWD ? 0 : inverse(p.HW);
             const float im0 = own_g < ge ? inv_hw / (float)(group_begin(p, own_g + 1) - group_begin(p, own_g)) : 0.f;
             if (p.cl > 1) sm100::cluster_barrier();
             else __syncthreads();
             // ---- the image's values from those of the cluster's blocks, in order
             for (int g = own_g; g < ge; g += p.threads) {
-                const float2 *v = xch + buf * p.cl * p.gs + (g - gb);
+                const Sum2 *v = xch + buf * p.cl * p.gs + (g - gb);
                 const int size = group_begin(p, g + 1) - group_begin(p, g);
                 const float im = g == own_g ? im0 : inv_hw / (float)size;
                 if (BWD) {
@@ -646,15 +728,20 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 } else {
                     // All blocks but the last have `share` pixels (those behind the last have none). Means are averaged as differences from the
                     // first block's, and the squares of what the blocks' means differ by belong to the variance.
-                    const float ref = v[0].x, last = rest > 0.f ? v[whole * p.gs].x - ref : 0.f;
-                    float d = 0.f, sq = 0.f;
-                    for (int r = 0; r < whole; ++r) { d += v[r * p.gs].x - ref; sq += v[r * p.gs].y; }
-                    if (rest > 0.f) sq += v[whole * p.gs].y;
-                    d = (d * (float)p.share + last * rest) * inv_hw;
-                    float spread = 0.f;
-                    for (int r = 0; r < whole; ++r) { const float o = v[r * p.gs].x - ref - d; spread = fmaf(o, o, spread); }
-                    spread = spread * (float)p.share + (last - d) * (last - d) * rest;
-                    const float fm = ref + d, fr = 1.f / sqrtf(fmaf(fmaf(spread, (float)size, sq), im, p.eps));
+                    const Sum ref = v[0].x;
+                    Sum d = 0, sq = 0, spread = 0;
+                    for (int r = 0; r < whole; ++r) {
+                        const Sum o = v[r * p.gs].x - ref;
+                        d += o; spread += o * o; sq += v[r * p.gs].y;
+                    }
+                    d *= p.share; spread *= p.share;
+                    if (rest > 0.f) {
+                        const Sum o = v[whole * p.gs].x - ref, n = o * rest;
+                        d += n; spread += n * o; sq += v[whole * p.gs].y;
+                    }
+                    spread -= d * d * inv_n;
+                    d *= inv_n;
+                    const float fm = (float)(ref + d), fr = 1.f / sqrtf((float)(spread * size + sq) * im + p.eps);
                     out[g] = fr;
                     out[p.G + g] = fm;
                     if (rank == 0) {
@@ -774,12 +861,12 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
         }
         if (BWD)                                                         // the images' sums of dz and dz * xhat, a channel's
             for (int c = v0 * 8 + t; c < min(p.C, (v0 + nv) * 8); c += p.threads) {
-                const float *src = red + ((c >> 3) - v0) * 17 + (c & 7);
+                const float *src = red + ((c >> 3) - v0) * kRed + (c & 7);
                 float w0 = 0.f, w1 = 0.f, u0 = 0.f, u1 = 0.f;
                 int r = 0;
-                for (; r + 1 < p.ppb; r += 2, src += 2 * p.rl * 17) {
+                for (; r + 1 < p.ppb; r += 2, src += 2 * p.rl * kRed) {
                     w0 += src[0]; w1 += src[8];
-                    u0 += src[p.rl * 17]; u1 += src[p.rl * 17 + 8];
+                    u0 += src[p.rl * kRed]; u1 += src[p.rl * kRed + 8];
                 }
                 if (r < p.ppb) { w0 += src[0]; w1 += src[8]; }
                 acc[c] += w0 + u0;
@@ -926,8 +1013,8 @@ size_t gn_shape(GnP *p, int mode, bool res, int cl)
     part(&p->sm_gam, (size_t)p->ld * 4);
     part(&p->sm_bet, (size_t)p->ld * 4);
     part(&p->sm_grp, (size_t)p->G * 6 * 4);
-    part(&p->sm_red, (size_t)p->threads * 17 * 4);
-    part(&p->sm_xch, (size_t)2 * cl * p->gs * 8);
+    part(&p->sm_red, (size_t)p->threads * gn_red(mode) * 4);
+    part(&p->sm_xch, (size_t)(cl > 1 ? 2 : 1) * cl * p->gs * (gn_bwd(mode) ? 8 : 16));
     part(&p->sm_acc, gn_bwd(mode) ? (size_t)2 * p->ld * 4 : 0);
     return at;
 }

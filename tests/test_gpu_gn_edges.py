@@ -30,3 +30,53 @@ def test_codes_of_a_pitch_that_passes_32_bits_within_a_block(npix, ldq):
     assert int(torch.count_nonzero(wide)) == int(torch.count_nonzero(dense))
     want = oracle.act_unpack(dense.cpu().numpy(), scales[:npix].cpu().numpy().reshape(npix, 1))
     assert np.array_equal(back.float().cpu().numpy().astype(np.float64), want)
+
+
+# ------------------------------------------------------------------------------------------------ statistics of the forward pass
+# A thread takes its pixels in runs and joins them. The k-th addition of a run is off by 2^-24 of the sum so far at most. The first run,
+# at most 16 pixels, is about the first of them: if that one is d away from equal others, the sum of squares grows by d^2 a step, so that
+# it is off by (1 + 2 + .. + 15) * 2^-24 d^2 = 7.2e-6 d^2, and the run's sum of squares about its mean is 15/16 d^2: 7.6e-6 of the
+# variance, 3.8e-6 of rstd = var^-1/2. (A first pixel that is no further away than others loses less: 16 * 2^-24.) The next run is about
+# the mean of the first, d/16 away: 48 * (d/16)^2 = 0.19 d^2 in 48 steps, 3e-7 of the variance; later ones less. 4e-6 holds rstd. A mean is
+# off by half of that at most, of the pixels' distances from the pivot: 4e-6 of the deviation, and a rounding of the mean to fp32.
+def _stats(x, G, copies, eps=1e-5, pack=False):
+    """rstd and mean of an image [H][W][C] of `copies` equal ones by the kernel, and in 64 bits; y of the last copy."""
+    c = Hh.ctx()
+    H, Wd, C = x.shape
+    xb = W.bf16_round(x)
+    xd = torch.zeros((copies, H, Wd, W.pad8(C)), dtype=torch.bfloat16, device="cuda")
+    xd[..., :C] = xb.bfloat16().cuda()
+    d = B.make_gn_desc(copies, H, Wd, C, G, eps=eps, act=B.PT_ACT_NONE)
+    mean, rstd = (torch.full((copies, G), 7.0, device="cuda") for _ in range(2))
+    y, one, zero = torch.empty_like(xd), torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    codes, scales = B.checkpoint_buffers(copies * H * Wd, C) if pack else (None, None)
+    B.pt_gn_act_fwd(c, d, xd, None, one, zero, mean, rstd, y, codes, scales)
+    torch.cuda.synchronize()
+    c.poll()
+    v = xb.double().reshape(H * Wd, G, C // G).permute(1, 0, 2).reshape(G, -1)
+    m = v.mean(1)
+    var = ((v - m[:, None]) ** 2).mean(1)
+    return mean.double().cpu(), rstd.double().cpu(), m, (var + eps).rsqrt(), var.sqrt(), y[-1, ..., :C].double().cpu(), xb.double()
+
+
+@pytest.mark.parametrize("base,odd", [(0.0, 100.0), (0.0, 1000.0), (10.0, 0.0), (1000.0, 0.0)])
+@pytest.mark.parametrize("H,C,G,copies", [(224, 8, 1, 300), (56, 64, 8, 2), (56, 1040, 4, 150), (112, 16, 2, 3)])
+def test_statistics_of_images_whose_first_pixels_are_unlike_the_rest(H, C, G, copies, base, odd):
+    """A border or a mask: one block per image and many, many pixels per thread and one."""
+    gen = torch.Generator().manual_seed(22)
+    x = base + torch.randn((H, H, C), generator=gen)
+    x.view(H * H, C)[:4] = odd
+    mean, rstd, m, r, dev, _, _ = _stats(x, G, copies, pack=base == 0.0)
+    assert float((rstd / r - 1).abs().max()) <= 4e-6
+    assert bool(((mean - m).abs() <= 4e-6 * dev + 2.0 ** -24 * m.abs()).all())
+
+
+@pytest.mark.parametrize("H,C,G,copies", [(30, 8, 1, 2), (30, 32, 2, 400), (5, 2040, 3, 2)])
+@pytest.mark.parametrize("at", [0, 1, 24])
+def test_one_step_in_a_constant_group_is_its_variance(H, C, G, copies, at):
+    """Every value 1000 but one, which is 1004, the next bf16: the variance is all in one thread's sums, or between its mean and the others'."""
+    x = torch.full((H, H, C), 1000.0)
+    x.view(H * H, G, C // G)[at, :, 0] = 1004.0
+    mean, rstd, m, r, dev, _, _ = _stats(x, G, copies, eps=0.0)
+    assert float((rstd / r - 1).abs().max()) <= 4e-6
+    assert bool(((mean - m).abs() <= 4e-6 * dev + 2.0 ** -24 * m.abs()).all())
