@@ -532,7 +532,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                         for (int h = 0; h < 2; ++h) {
                             const int j = 2 * i + h;
                             const float d = sum[h] * inv;
-                            sq[h] = fmaxf(fmaf(-sum[h], d, sq[h]), 0.f);
+                            sq[h] = fmaf(-sum[h], d, sq[h]);
+                            sq[h] = sq[h] < 0.f ? 0.f : sq[h];           // (a NaN stays)
                             off[h] = d;
                             if (taken > 0) {
                                 const float was = o[j], apart = d - was;
@@ -741,7 +742,9 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                     }
                     spread -= d * d * inv_n;
                     d *= inv_n;
-                    const float fm = (float)(ref + d), fr = 1.f / sqrtf((float)(spread * size + sq) * im + p.eps);
+                    // (squares that fp32 does not hold are an infinity or a NaN by now, and no variance)
+                    const float var = (float)((spread * size + sq) * (Sum)im);
+                    const float fm = (float)(ref + d), fr = var < INFINITY ? 1.f / sqrtf(var + p.eps) : __uint_as_float(0x7fc00000u);
                     out[g] = fr;
                     out[p.G + g] = fm;
                     if (rank == 0) {

@@ -80,3 +80,23 @@ def test_one_step_in_a_constant_group_is_its_variance(H, C, G, copies, at):
     mean, rstd, m, r, dev, _, _ = _stats(x, G, copies, eps=0.0)
     assert float((rstd / r - 1).abs().max()) <= 4e-6
     assert bool(((mean - m).abs() <= 4e-6 * dev + 2.0 ** -24 * m.abs()).all())
+
+
+@pytest.mark.parametrize("H,C,G,copies", [(20, 24, 3, 2), (20, 24, 3, 400), (3, 8, 1, 1)])
+@pytest.mark.parametrize("scale", [2.0 ** -50, 2.0 ** 49, 2.0 ** 64, 2.0 ** 80, 2.0 ** 125])
+def test_squares_at_the_ends_of_fp32(H, C, G, copies, scale):
+    """The largest and the smallest values that the header admits (|x| < 2^52: normal values below 8 times 2^49; a variance of 2^-100), as
+    they are; and larger ones: NaN where squares overflow, in the scaled group only, and nothing finite and wrong."""
+    gen = torch.Generator().manual_seed(23)
+    x = torch.randn((H, H, C), generator=gen)
+    x[..., :C // G] *= scale
+    mean, rstd, m, r, dev, y, xb = _stats(x, G, copies, eps=0.0)
+    over = torch.isnan(rstd)                       # (threads of one pixel have no squares of their own: 2^64 is right at 3x3)
+    assert not over[:, 1:].any() and not (scale < 2.0 ** 64 and over.any()) and (scale < 2.0 ** 80 or over[:, 0].all())
+    assert bool((over | ((rstd / r - 1).abs() <= 4e-6)).all())
+    assert bool((over | ((mean - m).abs() <= 4e-6 * dev + 2.0 ** -24 * m.abs())).all())
+    # y: its rounding to bf16, and 1e-5 of its terms, which are below 8
+    want = ((xb.reshape(H, H, G, -1) - m[:, None]) * r[:, None]).reshape(H, H, C)
+    gone = over[-1].repeat_interleave(C // G)
+    assert torch.isnan(y[..., gone]).all()
+    assert bool(((y - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5 * 8)[..., ~gone].all())
