@@ -270,7 +270,8 @@ pt_status pt_bn_relu_bwd(pt_ctx *ctx, const pt_bn_desc *d, const void *x, const 
  * as an input of its call (y as x or residual; dx and dresidual as x, residual or dy, but not as each other); otherwise no two overlap.
  * An infinity or a NaN in x makes the outputs of its image and group NaN; a NaN in the residual stays in its element of y. The forward pass
  * wants |x| below 2^52 and var + eps above 2^-100: its squares are fp32. Where larger ones overflow, the outputs of the image and group are
- * NaN; smaller ones lose bits, and groups of equal values have no rstd where eps is 0. PT_ACT_SILU wants
+ * NaN; smaller ones lose bits, and groups of equal values have no rstd where eps is 0. The backward passes take rstd from 2^-60 to 2^60.
+ * PT_ACT_SILU wants
  * |gamma*xhat + beta| below 2^30 and a residual below 2^126 (it may be as low as the type goes, and leaves 0 then).
  * The current device must be the context's. PT_ERR_INVALID_ARG for bad sizes, pitches, alignment, groups, missing pointers or another
  * current device; PT_ERR_UNSUPPORTED for ld > 2048, more than 2^24 images, an image of 4 GB or

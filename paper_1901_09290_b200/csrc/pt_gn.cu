@@ -723,7 +723,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
                 if (BWD) {
                     float e0 = 0.f, e1 = 0.f;
                     for (int r = 0; r < p.cl; ++r) { e0 += v[r * p.gs].x; e1 += v[r * p.gs].y; }
-                    const float rs = grp[p.G + g], t1 = -(rs * rs * rs * e1 * im);
+                    const float rs = grp[p.G + g], t1 = -(rs * (rs * (rs * (e1 * im))));     // (rs^3 by itself may not be an fp32 number)
                     out[g] = -(rs * e0 * im);
                     out[p.G + g] = t1;
                 } else {

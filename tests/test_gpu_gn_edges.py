@@ -100,3 +100,52 @@ def test_squares_at_the_ends_of_fp32(H, C, G, copies, scale):
     gone = over[-1].repeat_interleave(C // G)
     assert torch.isnan(y[..., gone]).all()
     assert bool(((y - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5 * 8)[..., ~gone].all())
+
+
+# ------------------------------------------------------------------------------------------------ gradients
+def _backward(x, dy, g, b, mean, rstd, begin, act, res=None, packed=False, want_dres=True):
+    """dx, dresidual, dgamma, dbeta of x [N][H][W][C] (C a multiple of 8) by the kernel, as fp64."""
+    c = Hh.ctx()
+    N, H, Wd, C = x.shape
+    G = len(begin) - 1
+    d = B.make_gn_desc(N, H, Wd, C, G, C, act=act, group_begin=begin)
+    f = lambda a: torch.as_tensor(np.asarray(a), dtype=torch.float32).cuda()
+    xd, dyd, rd = x.bfloat16().cuda(), dy.bfloat16().cuda(), res.bfloat16().cuda() if res is not None else None
+    dx, dres = torch.empty_like(xd), torch.empty_like(xd) if want_dres else None
+    dg, db = (torch.full((C,), 7.0, device="cuda") for _ in range(2))
+    ws = torch.empty(B.pt_gn_workspace_bytes(c, d), dtype=torch.uint8, device="cuda")
+    if packed:
+        codes, scales = B.checkpoint_buffers(N * H * Wd, C)
+        B.pt_act_pack(c, B.make_pack_desc(N * H * Wd, C), xd, codes, scales)
+        B.pt_gn_act_bwd_packed(c, d, codes, scales, rd, dyd, f(g), f(b), f(mean), f(rstd), dx, dres, dg, db, None, ws)
+    else:
+        B.pt_gn_act_bwd(c, d, xd, rd, dyd, f(g), f(b), f(mean), f(rstd), dx, dres, dg, db, ws)
+    torch.cuda.synchronize()
+    c.poll()
+    h = lambda t: t.double().cpu().numpy() if t is not None else None
+    return h(dx), h(dres), h(dg), h(db)
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("rstd", [2.0 ** -60, 2.0 ** -50, 1e-13, 1e13, 2.0 ** 50, 2.0 ** 60])
+def test_gradients_at_small_and_large_deviations(rstd, packed, act):
+    """dx keeps its term in xhat where rstd^3 is not an fp32 number. The bound is that of ordinary values: a rounding to bf16 and 1e-5 of the
+    terms' magnitudes."""
+    gen = torch.Generator().manual_seed(24)
+    N, H, C, begin = 2, 9, 24, [0, 11, 24]
+    x = W.bf16_round(torch.randn((N, H, H, C), generator=gen) / rstd)
+    dy, g, b = W.bf16_round(torch.randn((N, H, H, C), generator=gen)), torch.rand(C, generator=gen) + 0.5, torch.rand(C, generator=gen) - 0.5
+    _, mean, _ = oracle.gn_act_fwd(x.numpy(), g.numpy(), b.numpy(), begin, 0.0)
+    mean, rs = mean.astype(np.float32), np.full((N, 2), rstd, np.float32)
+    dx, _, dg, db = _backward(x, dy, g, b, mean, rs, begin, act, packed=packed)
+    xv = oracle.act_unpack(*oracle.act_pack(x.numpy())) if packed else x.double().numpy()
+    rdx, _, rdg, rdb, _ = oracle.gn_act_bwd(xv, dy.numpy(), g.numpy(), b.numpy(), mean, rs, begin, None, act)
+    sp = lambda v: np.repeat(np.asarray(v, np.float64), np.diff(begin), axis=1)[:, None, None, :]
+    xhat, w = np.abs(xv - sp(mean)) * sp(rs), np.abs(dy.double().numpy() * g.double().numpy()) * (1.1 if act == 2 else 1.0)
+    # (SiLU's slope is 1.1 at most)
+    means = lambda v: sp(np.stack([v[..., s:e].mean((1, 2, 3)) for s, e in zip(begin[:-1], begin[1:])], 1))
+    terms = sp(rs) * (w + means(w) + xhat * means(w * xhat))
+    assert np.all(np.abs(dx - rdx) <= 2.0 ** -8 * np.abs(rdx) + 1e-5 * terms)
+    ady = np.abs(dy.double().numpy()) * 1.1
+    assert np.all(np.abs(dg - rdg) <= 1e-5 * (ady * xhat).sum((0, 1, 2))) and np.all(np.abs(db - rdb) <= 1e-5 * ady.sum((0, 1, 2)))
