@@ -35,6 +35,7 @@ constexpr int kGnMaxN = 1 << 24;             // most images: units, and steps be
 constexpr int kGnMaxCluster = 16;
 constexpr int kGnExchange = 1024;            // most entries (blocks of the cluster x groups) of one exchange buffer
 constexpr int kGnSlabs = 32;                 // most slabs of channels
+constexpr int kGnChain = 32;                 // units whose sums for dgamma and dbeta are added up in fp32
 
 enum { kGnFwd = 0, kGnFwdPack = 1, kGnBwd = 2, kGnBwdPacked = 3 };
 
@@ -74,6 +75,7 @@ struct GnArgs {
     uint4 *y, *dx, *dres;
     uint8_t *codes, *scales;
     float *rows;                 // backward: [blocks][2][ld] sums of dz and dz * xhat over a block's units
+    double *wide;                // [blocks][2][ld] those of all but its last few units
     float *dgamma, *dbeta;
 };
 
@@ -199,6 +201,16 @@ __device__ __noinline__ uint32_t exact_mask(uint32_t x, uint32_t r, int c, const
     return m;
 }
 
+// A block's sums on to its own in 64 bits; the first time they are what those hold. Out of line: rarely called.
+__device__ __noinline__ void empty_sums(double *wide, float *acc, int n, bool first)
+{
+    double *row = wide + (size_t)blockIdx.x * n;
+    for (int e = threadIdx.x; e < n; e += blockDim.x) {
+        row[e] = (first ? 0.0 : row[e]) + (double)acc[e];
+        acc[e] = 0.f;
+    }
+}
+
 // Eight restored values as pairs (act8::decode8), and two of them as bf16, in which they are exact: their upper halves.
 __device__ __forceinline__ void decode8(const uint2 &q, uint32_t byte, f2 (&x)[4])
 {
@@ -243,7 +255,7 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     float *out = grps + 4 * p.G;                                         // [2][G] rstd and mean (forward), the group's terms of dx (backward)
     float *red = reinterpret_cast<float *>(smem + p.sm_red);             // [threads][kRed]
     Sum2 *xch = reinterpret_cast<Sum2 *>(smem + p.sm_xch);               // [2][cl][gs], of alternating images; one without clusters
-    float *acc = reinterpret_cast<float *>(smem + p.sm_acc);             // [2][ld] the block's sums of dz and dz * xhat over its units
+    float *acc = reinterpret_cast<float *>(smem + p.sm_acc);             // [2][ld] sums of dz and dz * xhat over the block's last units
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = p.threads >> 5;
     const int rank = (int)(blockIdx.x % p.cl), cluster = (int)(blockIdx.x / p.cl);
     const int first = rank * p.share, mine = p.HW - first < p.share ? (p.HW - first > 0 ? p.HW - first : 0) : p.share;
@@ -344,6 +356,10 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     const int whole = p.HW / p.share;                                    // blocks with all their pixels
     const float rest = (float)(p.HW - whole * p.share);                  // pixels of the one behind them
     while (n < p.N) {
+        if (BWD && it > 0 && it % kGnChain == 0) {                       // (here: at the loop's end it would cost registers)
+            __syncthreads();
+            empty_sums(a.wide, acc, 2 * p.ld, it == kGnChain);
+        }
         int next_n = n + p.step_n, next_s = sl + p.step_s;
         if (next_s >= p.slabs) { next_s -= p.slabs; next_n += 1; }
         const bool more = next_n < p.N;
@@ -880,17 +896,19 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
     // ---- the block's row of sums
     if (BWD) {
         __syncthreads();
+        const size_t own = (size_t)blockIdx.x * 2 * p.ld;
         for (int e = t; e < 2 * p.ld; e += p.threads) {
             const int s = e >= p.ld, c = e - s * p.ld;
-            if (gridDim.x > 1) a.rows[(size_t)blockIdx.x * 2 * p.ld + e] = acc[e];
-            else if (c < p.C) (s ? a.dgamma : a.dbeta)[c] = acc[e];
+            const float v = it > kGnChain ? (float)(a.wide[own + e] + (double)acc[e]) : acc[e];
+            if (gridDim.x > 1) a.rows[own + e] = v;
+            else if (c < p.C) (s ? a.dgamma : a.dbeta)[c] = v;
         }
     }
 }
 
 // dgamma, dbeta: the blocks' rows. A block owns 32 columns; a warp adds every 32nd row of them, all loads before the first addition, then
-// a column's 32 sums: a fixed order, chains of at most ten. (Plain loads: the rows are still being written when this kernel starts, so they
-// are not read-only for all of its life.)
+// a column's 32 sums: a fixed order, chains of at most ten. (In 64 bits the backward pass of 64x14x14x931 from a checkpoint takes 43.7 us
+// for 43.3.) Plain loads: the rows are still being written when this kernel starts, so they are not read-only for all of its life.
 __global__ void __launch_bounds__(1024) gn_finish_kernel(const float *rows, int n, int C, int ld, float *dgamma, float *dbeta)
 {
     __shared__ float part[32][33];
@@ -1162,14 +1180,16 @@ pt_status launch_gn(pt_ctx *c, const GnP &key, const GnArgs &a, int mode, int ac
     return PT_OK;
 }
 
+// Sums of dz and dz * xhat in the workspace: a row per block.
+size_t gn_sums(const pt_ctx *c, const GnP &p) { return (size_t)c->sm_count * kGnBlocks * 2 * p.ld; }
+
 }  // namespace
 
 extern "C" size_t pt_gn_workspace_bytes(const pt_ctx *c, const pt_gn_desc *d)
 {
     GnP p;
     if (gn_params(c, d, false, &p) != PT_OK) return 0;
-    // a row of sums per block
-    return (size_t)c->sm_count * kGnBlocks * 2 * p.ld * sizeof(float);
+    return gn_sums(c, p) * (sizeof(double) + sizeof(float));
 }
 
 extern "C" pt_status pt_gn_act_fwd(pt_ctx *c, const pt_gn_desc *d, const void *x, const void *residual, const float *gamma, const float *beta,
@@ -1199,7 +1219,7 @@ extern "C" pt_status pt_gn_act_bwd(pt_ctx *c, const pt_gn_desc *d, const void *x
     GnArgs a{};
     a.x = (const uint4 *)x; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy; a.gamma = gamma; a.beta = beta; a.mean = save_mean;
     a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual;
-    a.rows = (float *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.wide = (double *)ws; a.rows = (float *)(a.wide + gn_sums(c, p)); a.dgamma = dgamma; a.dbeta = dbeta;
     return launch_gn(c, p, a, kGnBwd, d->act, (cudaStream_t)stream);
 }
 
@@ -1217,6 +1237,6 @@ extern "C" pt_status pt_gn_act_bwd_packed(pt_ctx *c, const pt_gn_desc *d, const 
     GnArgs a{};
     a.codes_in = (const uint8_t *)codes; a.scales_in = (const uint8_t *)scales; a.res = (const uint4 *)residual; a.dy = (const uint4 *)dy;
     a.gamma = gamma; a.beta = beta; a.mean = save_mean; a.rstd = save_rstd; a.dx = (uint4 *)dx; a.dres = (uint4 *)dresidual; a.y = (uint4 *)y;
-    a.rows = (float *)ws; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.wide = (double *)ws; a.rows = (float *)(a.wide + gn_sums(c, p)); a.dgamma = dgamma; a.dbeta = dbeta;
     return launch_gn(c, p, a, kGnBwdPacked, d->act, (cudaStream_t)stream);
 }

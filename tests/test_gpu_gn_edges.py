@@ -149,3 +149,35 @@ def test_gradients_at_small_and_large_deviations(rstd, packed, act):
     assert np.all(np.abs(dx - rdx) <= 2.0 ** -8 * np.abs(rdx) + 1e-5 * terms)
     ady = np.abs(dy.double().numpy()) * 1.1
     assert np.all(np.abs(dg - rdg) <= 1e-5 * (ady * xhat).sum((0, 1, 2))) and np.all(np.abs(db - rdb) <= 1e-5 * ady.sum((0, 1, 2)))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("N", [33 * 296 + 5, 1 << 20, 1 << 24])
+def test_parameter_gradients_over_many_small_images(N, packed):
+    """Images of one pixel with equal gradients of one sign: chains of equal additions, which fp32 rounds the same way every time. 32 units are
+    added in fp32, off by 2^-24 of their sum so far each, (1 + .. + 32)/32 * 2^-24 = 1e-6 of the sum; a product of rounded factors before
+    them adds 3 * 2^-24, the rounding of a block's sum 2^-24; the sums of at most 320 blocks are added ten in a row, (1 + .. + 9)/10 * 2^-24,
+    and those in five steps, 5 * 2^-24: 1.9e-6 in all."""
+    C, begin = 8, [0, 3, 8]
+    x, dy = torch.full((N, 1, 1, C), 1.5), torch.full((N, 1, 1, C), 0.69921875)
+    mean, rstd = np.full((N, 2), 0.3, np.float32), np.full((N, 2), 0.9, np.float32)
+    _, _, dg, db = _backward(x, dy, np.ones(C), np.ones(C), mean, rstd, begin, 1, packed=packed, want_dres=False)
+    xhat = (1.5 - float(np.float32(0.3))) * float(np.float32(0.9))
+    assert np.abs(db / (N * 0.69921875) - 1).max() <= 1.9e-6
+    assert np.abs(dg / (N * 0.69921875 * xhat) - 1).max() <= 1.9e-6
+
+
+def test_one_call_for_many_images_is_many_calls():
+    """dgamma and dbeta of a batch whose blocks take dozens of images each are the sums of the batch's parts, which take a few."""
+    gen = torch.Generator().manual_seed(25)
+    N, H, C, begin = 24000, 2, 16, [0, 5, 16]
+    x, dy = W.bf16_round(torch.randn((N, H, H, C), generator=gen)), W.bf16_round(torch.randn((N, H, H, C), generator=gen).abs())
+    g, b = torch.rand(C, generator=gen) + 0.5, torch.rand(C, generator=gen) - 0.5
+    mean, rstd = np.zeros((N, 2), np.float32), np.ones((N, 2), np.float32)
+    dx, _, dg, db = _backward(x, dy, g, b, mean, rstd, begin, 2)
+    parts = [_backward(x[s:s + 2000], dy[s:s + 2000], g, b, mean[s:s + 2000], rstd[s:s + 2000], begin, 2) for s in range(0, N, 2000)]
+    assert np.array_equal(dx, np.concatenate([q[0] for q in parts]))
+    ady = dy.double().numpy() * 1.1                             # (SiLU's slope is 1.1 at most)
+    # both sides: 1.9e-6 of the magnitudes as above, and SiLU's slope, off the same way on both
+    assert np.all(np.abs(dg - sum(q[2] for q in parts)) <= 3.8e-6 * (ady * np.abs(x.double().numpy())).sum((0, 1, 2)))
+    assert np.all(np.abs(db - sum(q[3] for q in parts)) <= 3.8e-6 * ady.sum((0, 1, 2)))
