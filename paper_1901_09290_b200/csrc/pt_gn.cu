@@ -168,21 +168,39 @@ __device__ __forceinline__ uint32_t bf16_floor(float v)
     return (u >> 31) ? ((u + 0xffffu) >> 16) : (u >> 16);                // (towards -inf: a negative one's magnitude rounds up)
 }
 
+__device__ __forceinline__ double exact_z(double x, float mean, float rstd, float gamma, float beta) { return (x - (double)mean) * (double)rstd * (double)gamma + (double)beta; }
+
 // ReLU without a residual: z = s*(x - mean) + beta > 0, s = gamma*rstd, for bf16 x, as sg ^ x > th. For s > 0 that is x > mean - beta/s, for
-// s < 0 -x > -(mean - beta/s), for s = 0 a constant. What fp32 leaves uncertain of the limit hardly ever lies about a bf16 value, and then
-// 64 bits decide.
-__device__ __noinline__ uint32_t relu_limit_exact(float mean, float rstd, float gamma, float beta)         // th, and sg above it
+// s < 0 -x > -(mean - beta/s), for s = 0 a constant. What fp32 leaves uncertain of the limit hardly ever lies about a bf16 value; where it
+// does, or is out of range, z at the bf16 values themselves decides, in 64 bits. (A limit in 64 bits would not: beta may be lost beside the
+// mean.) z rises with sg ^ x, so that a bisection finds the last value without z > 0: of the bf16 values in their order, number_of, between
+// lo, which is such a value, and hi, which is none unless it is infinity.
+__device__ __forceinline__ uint32_t number_of(uint32_t bits) { return bits & 0x8000u ? ~bits & 0xffffu : bits | 0x8000u; }
+constexpr uint32_t kLowest = 0x7fu, kHighest = 0xff80u;                  // -inf and inf
+__device__ __noinline__ uint32_t relu_limit_exact(float mean, float rstd, float gamma, float beta, uint32_t lo, uint32_t hi)     // th, and sg above it
 {
-    const double sd = (double)gamma * (double)rstd, ld = (double)mean - (double)beta / sd;
-    return bf16_floor(__double2float_rd(sd == 0.0 ? (beta > 0.f ? -INFINITY : INFINITY) : sd < 0.0 ? -ld : ld)) | (sd < 0.0 ? 0x80000000u : 0u);
+    const double sd = (double)gamma * (double)rstd;
+    if (sd == 0.0) return beta > 0.f ? 0xff80u : 0x7f80u;
+    const uint32_t flip = sd < 0.0 ? 0x8000u : 0u;
+    const auto bits_of = [](uint32_t i) { return i & 0x8000u ? i ^ 0x8000u : ~i & 0xffffu; };
+    const auto above = [&](uint32_t i) { return exact_z((double)__uint_as_float((bits_of(i) ^ flip) << 16), mean, rstd, gamma, beta) > 0.0; };
+    if (hi == kHighest && !above(hi)) lo = hi;                           // (statistics that are NaN)
+    while (lo + 1u < hi) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (above(mid)) hi = mid;
+        else lo = mid;
+    }
+    return bits_of(lo) | flip << 16;
 }
 __device__ __forceinline__ void relu_limit(float mean, float rstd, float gamma, float beta, uint32_t &th, uint32_t &sg)
 {
     const float s = gamma * rstd, q = __fdividef(beta, s), lim = s < 0.f ? q - mean : mean - q, off = 1e-6f * (fabsf(mean) + fabsf(q));
+    const bool in_range = fabsf(lim) > 1e-30f && fabsf(lim) < 1e30f && fabsf(s) > 1e-30f && fabsf(s) < 1e30f;
     sg = s < 0.f ? 0x8000u : 0u;
     th = bf16_floor(lim - off);
-    if (th != bf16_floor(lim + off) || !(fabsf(lim) < 1e30f) || !(fabsf(s) > 1e-30f && fabsf(s) < 1e30f)) {
-        th = relu_limit_exact(mean, rstd, gamma, beta);
+    const uint32_t up = bf16_floor(lim + off);
+    if (th != up || !in_range) {
+        th = relu_limit_exact(mean, rstd, gamma, beta, in_range ? number_of(th) : kLowest, in_range ? number_of(up) + 1u : kHighest);
         sg = th >> 16;
         th &= 0xffffu;
     }
@@ -196,7 +214,7 @@ __device__ __noinline__ uint32_t exact_mask(uint32_t x, uint32_t r, int c, const
     for (int h = 0; h < 2; ++h) {
         const int g = gid[c + h];
         const double xv = (double)__uint_as_float(h ? x & 0xffff0000u : x << 16), rv = (double)__uint_as_float(h ? r & 0xffff0000u : r << 16);
-        if ((xv - (double)grp[g]) * (double)grp[G + g] * (double)gam[c + h] + (double)bet[c + h] + rv > 0.0) m |= h ? 0xffff0000u : 0xffffu;
+        if (exact_z(xv, grp[g], grp[G + g], gam[c + h], bet[c + h]) + rv > 0.0) m |= h ? 0xffff0000u : 0xffffu;
     }
     return m;
 }

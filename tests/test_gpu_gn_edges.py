@@ -181,3 +181,43 @@ def test_one_call_for_many_images_is_many_calls():
     # both sides: 1.9e-6 of the magnitudes as above, and SiLU's slope, off the same way on both
     assert np.all(np.abs(dg - sum(q[2] for q in parts)) <= 3.8e-6 * (ady * np.abs(x.double().numpy())).sum((0, 1, 2)))
     assert np.all(np.abs(db - sum(q[3] for q in parts)) <= 3.8e-6 * ady.sum((0, 1, 2)))
+
+
+@pytest.mark.parametrize("with_res", [False, True])
+@pytest.mark.parametrize("packed", [False, True])
+def test_relu_where_beta_is_lost_beside_the_mean(packed, with_res):
+    """A group of equal values is its beta: of either sign, however small beside the mean, with either sign of gamma and without one, z > 0
+    exactly where beta > 0."""
+    N, H, C = 2, 4, 32
+    gen = torch.Generator().manual_seed(26)
+    beta = torch.tensor([1e-12, -1e-12, 1e-4, -1e-4, 2.0 ** -100, -(2.0 ** -100), 0.0, -0.0]).repeat(4)
+    gamma = torch.tensor([1.0, -1.0, 0.75, 0.0]).repeat_interleave(8)
+    for value in (1000.0, -0.5, 0.0):
+        x, dy = torch.full((N, H, H, C), value), W.bf16_round(torch.rand((N, H, H, C), generator=gen) + 0.5)
+        res = torch.zeros_like(x) if with_res else None
+        dx, dres, dg, db = _backward(x, dy, gamma, beta, np.full((N, 1), value, np.float32), np.full((N, 1), 1e-5 ** -0.5, np.float32), [0, C], 1, res, packed)
+        want = dy.double().numpy() * (beta.numpy() > 0)
+        assert np.array_equal(dres, want), value
+        assert np.all(np.abs(db - want.sum((0, 1, 2))) <= 1e-6 * want.sum((0, 1, 2)))
+
+
+@pytest.mark.parametrize("with_res", [False, True])
+def test_relu_next_to_its_limit(with_res):
+    """beta is minus gamma * xhat of a value, rounded to fp32: z there is its rounding, 2^-25 of beta or less, and the next bf16 values lie on
+    either side. Against the formula in 64 bits, which is off by 2^-52 of beta."""
+    gen = torch.Generator().manual_seed(27)
+    N, H, C = 1, 3, 2048
+    for mean, scale in ((0.0, 1.0), (3.14159, 1.0), (100.3, 0.01), (-7.7, 1e-6), (1e-3, 1e4)):
+        mean, rstd = np.full((N, 1), mean, np.float32), np.full((N, 1), 1.37 / scale, np.float32)
+        gamma = torch.where(torch.rand(C, generator=gen) < 0.5, -1.0, 1.0) * (torch.rand(C, generator=gen) + 0.1)
+        at = W.bf16_round(torch.from_numpy(mean.astype(np.float32))[0] + scale * torch.randn(C, generator=gen))
+        xhat = (at.double() - float(mean[0, 0])) * float(rstd[0, 0])
+        beta = -(xhat * gamma.double()).float()
+        bits = at.bfloat16().view(torch.int16).to(torch.int32)
+        x = torch.stack([(bits + k).to(torch.int16).view(torch.bfloat16).float() for k in (-2, -1, -1, 0, 0, 0, 1, 1, 2)]).view(N, H, H, C)
+        dy = torch.ones((N, H, H, C))
+        res = torch.zeros_like(x) if with_res else None
+        _, dres, _, db = _backward(x, dy, gamma, beta, mean, rstd, [0, C], 1, res)
+        z = (x.double() - float(mean[0, 0])) * float(rstd[0, 0]) * gamma.double() + beta.double()
+        assert np.array_equal(dres > 0, (z > 0).numpy())
+        assert np.array_equal(db, (z > 0).sum((0, 1, 2)).double().numpy())
