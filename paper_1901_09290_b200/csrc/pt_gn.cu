@@ -494,10 +494,8 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         // (gamma = 0, a pruned channel's or a pad lane's: z = beta + residual, of the right sign in fp32)
-                        float k0, k1;
-                        un2(k[i], k0, k1);
-                        const bool near0 = k0 != 0.f && fabsf(zz[2 * i]) <= fmaf(fabsf(__uint_as_float(rb[i] << 16)), 1e-6f, be_max);
-                        const bool near1 = k1 != 0.f && fabsf(zz[2 * i + 1]) <= fmaf(fabsf(__uint_as_float(rb[i] & 0xffff0000u)), 1e-6f, be_max);
+                        const bool near0 = gam[c0 + 2 * i] != 0.f && fabsf(zz[2 * i]) <= fmaf(fabsf(__uint_as_float(rb[i] << 16)), 1e-6f, be_max);
+                        const bool near1 = gam[c0 + 2 * i + 1] != 0.f && fabsf(zz[2 * i + 1]) <= fmaf(fabsf(__uint_as_float(rb[i] & 0xffff0000u)), 1e-6f, be_max);
                         uint32_t m = (zz[2 * i] > 0.f ? 0xffffu : 0u) | (zz[2 * i + 1] > 0.f ? 0xffff0000u : 0u);
                         if (near0 || near1) m = exact_mask(xb[i], rb[i], c0 + 2 * i, gid, grp, p.G, gam, bet);
                         g[i] &= m;

@@ -221,3 +221,18 @@ def test_relu_next_to_its_limit(with_res):
         z = (x.double() - float(mean[0, 0])) * float(rstd[0, 0]) * gamma.double() + beta.double()
         assert np.array_equal(dres > 0, (z > 0).numpy())
         assert np.array_equal(db, (z > 0).sum((0, 1, 2)).double().numpy())
+
+
+@pytest.mark.parametrize("with_res", [False, True])
+@pytest.mark.parametrize("packed", [False, True])
+def test_relu_where_gamma_times_rstd_is_no_fp32_number(packed, with_res):
+    """z = gamma * xhat, of the sign of x - mean, where gamma * rstd underflows to 0 in fp32; a gamma of 0 passes nothing."""
+    gen = torch.Generator().manual_seed(28)
+    N, H, C = 2, 5, 16
+    x = W.bf16_round(torch.randn((N, H, H, C), generator=gen) * 2.0 ** 50)
+    dy, gamma = torch.ones((N, H, H, C)), torch.tensor([1e-38, -1e-38, 1e-40, 0.0]).repeat(4)
+    mean, rstd = np.zeros((N, 1), np.float32), np.full((N, 1), 2.0 ** -50, np.float32)
+    _, dres, _, db = _backward(x, dy, gamma, np.zeros(C), mean, rstd, [0, C], 1, torch.zeros_like(x) if with_res else None, packed)
+    xv = oracle.act_unpack(*oracle.act_pack(x.numpy())) if packed else x.double().numpy()
+    want = xv * np.sign(gamma.double().numpy()) > 0
+    assert np.array_equal(dres > 0, want) and np.array_equal(db, want.sum((0, 1, 2)))
