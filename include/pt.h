@@ -304,10 +304,11 @@ typedef struct {
     int32_t C, ld;     /* channels, pitch of the bf16 tensor (elements, multiple of 8, >= C, <= 2048) */
     int32_t ldq;       /* pitch of the codes (bytes, multiple of 8, >= C) */
 } pt_pack_desc;
-/* Bytes to allocate for the scales of a checkpoint: npix * ceil(C/32), rounded up to a multiple of 16 (0 for invalid arguments). */
+/* Bytes to allocate for the scales of a checkpoint: npix * ceil(C/32), rounded up to a multiple of 16 (0 for arguments that the calls below
+ * refuse). */
 size_t pt_act_scale_bytes(int64_t npix, int32_t C);
 /* x (bf16 [npix][ld]) into a checkpoint, and a checkpoint into x (pad lanes written as zeros). PT_ERR_INVALID_ARG for bad sizes,
- * pitches, alignment, null pointers or a current device other than the context's; PT_ERR_UNSUPPORTED for ld > 2048. */
+ * pitches, alignment, null pointers or a current device other than the context's; PT_ERR_UNSUPPORTED for ld > 2048 or more than 2^40 pixels. */
 pt_status pt_act_pack(pt_ctx *ctx, const pt_pack_desc *d, const void *x, void *codes, void *scales, void *stream);
 pt_status pt_act_unpack(pt_ctx *ctx, const pt_pack_desc *d, const void *codes, const void *scales, void *x, void *stream);
 

@@ -991,7 +991,8 @@ pt_status gn_params(const pt_ctx *c, const pt_gn_desc *d, bool codes, GnP *p)
     }
     if (d->N > kGnMaxN || d->ld > kGnMaxLd || (p->table && d->groups > kGnTable)) return PT_ERR_UNSUPPORTED;
     const long long hw = (long long)d->H * d->W;
-    if (hw * d->ld * 2 >= 0x100000000ll || (codes && hw * d->ldq >= 0x100000000ll)) return PT_ERR_UNSUPPORTED;    // (offsets in an image have 32 bits)
+    // (offsets in an image have 32 bits; first the pixels alone, so that the products have fewer than 64)
+    if (hw >= 0x80000000ll || hw * d->ld * 2 >= 0x100000000ll || (codes && hw * d->ldq >= 0x100000000ll)) return PT_ERR_UNSUPPORTED;
     if (p->table)
         for (int g = 0; g <= d->groups; ++g) p->begin[g] = (uint16_t)b[g];
     p->N = d->N; p->HW = (int)hw; p->C = d->C; p->ld = d->ld; p->LV = d->ld / 8; p->ldq = d->ldq; p->nb = pt_ceil_div(d->C, act8::kBlock);

@@ -9,7 +9,7 @@
 namespace {
 
 constexpr int kPackThreads = 256;
-
+constexpr long long kMaxPixels = 1ll << 40;      // more than any memory holds: products with pitches stay within 64 bits
 constexpr int kPackBlocks = 6;      // thread blocks of an SM at a time
 
 struct PackP {
@@ -100,7 +100,7 @@ pt_status pack_params(const pt_ctx *c, const pt_pack_desc *d, const void *x, con
     if (d->npix < 0 || d->C < 1 || d->ld < d->C || (d->ld & 7) || d->ldq < d->C || (d->ldq & 7)) return PT_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)codes | (uintptr_t)scales) & 15) return PT_ERR_INVALID_ARG;
     if (!pt_on_device(c)) return PT_ERR_INVALID_ARG;
-    if (d->ld > 2048) return PT_ERR_UNSUPPORTED;
+    if (d->ld > 2048 || d->npix > kMaxPixels) return PT_ERR_UNSUPPORTED;
     p->npix = d->npix; p->C = d->C; p->ld = d->ld; p->ldq = d->ldq;
     p->LV = (d->C + 7) / 8; p->nb = pt_ceil_div(d->C, act8::kBlock);
     p->w = p->LV >= 3 ? 4 : p->LV;
@@ -111,8 +111,8 @@ pt_status pack_params(const pt_ctx *c, const pt_pack_desc *d, const void *x, con
 
 extern "C" size_t pt_act_scale_bytes(int64_t npix, int32_t C)
 {
-    if (npix < 0 || C < 1) return 0;
-    return pt_align_up((size_t)npix * (size_t)((C + act8::kBlock - 1) / act8::kBlock), 16);
+    if (npix < 0 || npix > kMaxPixels || C < 1 || C > 2048) return 0;
+    return pt_align_up((size_t)npix * (size_t)pt_ceil_div(C, act8::kBlock), 16);
 }
 
 extern "C" pt_status pt_act_pack(pt_ctx *c, const pt_pack_desc *d, const void *x, void *codes, void *scales, void *stream)

@@ -236,3 +236,22 @@ def test_relu_where_gamma_times_rstd_is_no_fp32_number(packed, with_res):
     xv = oracle.act_unpack(*oracle.act_pack(x.numpy())) if packed else x.double().numpy()
     want = xv * np.sign(gamma.double().numpy()) > 0
     assert np.array_equal(dres > 0, want) and np.array_equal(db, want.sum((0, 1, 2)))
+
+
+# ------------------------------------------------------------------------------------------------ refusals
+def test_sizes_whose_products_pass_64_bits_are_refused():
+    c = Hh.ctx()
+    t, v, s = torch.zeros(64, dtype=torch.bfloat16, device="cuda"), torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda")
+    most = (1 << 31) - 1
+    for H, Wd in ((most, most), (most, 1 << 30), (1 << 30, 1 << 30), (1 << 16, 1 << 15)):
+        d = B.make_gn_desc(1, H, Wd, 8, 1, 8)
+        assert B.pt_gn_workspace_bytes(c, d) == 0, (H, Wd)
+        with pytest.raises(B.PtError) as e:
+            B.pt_gn_act_fwd(c, d, t, None, v, v, s, s.clone(), t.clone())
+        assert e.value.status == 2
+    codes, scales = B.checkpoint_buffers(4, 8)
+    for npix in ((1 << 40) + 1, (1 << 63) - 1):
+        for call in (lambda d: B.pt_act_pack(c, d, t, codes, scales), lambda d: B.pt_act_unpack(c, d, codes, scales, t)):
+            with pytest.raises(B.PtError) as e:
+                call(B.make_pack_desc(npix, 8))
+            assert e.value.status == 2
