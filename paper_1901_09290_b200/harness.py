@@ -837,7 +837,8 @@ class CheckpointedStep(ChainedStep):
     """The chain with group normalisation that keeps its activations in 8 bits between the passes. A layer keeps the checkpoint of its
     convolution's output and nothing else: the backward pass of its normalisation restores the activation that the next convolution's
     weight gradient reads. Blocks keep the checkpoints of their input and, behind a projection, of the shortcut. Convolution outputs and
-    activations live in a few buffers that all layers share."""
+    activations live in buffers that all layers share, up to 16 of the size of the largest activation: a network of few layers needs more
+    memory this way than with a buffer for every tensor."""
 
     keeps_tensors = False
 
@@ -947,6 +948,9 @@ class CheckpointedStep(ChainedStep):
         self._filters(0, self.x0, self._norm_bwd(0, None, d_cur, None, None, "dy0", stream), stream)
 
     def saved_bytes(self) -> int:
-        """What stays between the forward and the backward pass of a step: the checkpoints and the statistics."""
+        """What stays between the forward and the backward pass of a step: the checkpoints, the statistics and, behind a pooled stem, the
+        positions that the pooling took. Not in it: the shared buffers, in which neither pass leaves anything for the other, though they stay
+        allocated."""
         pairs = list(self.ck.values()) + [s[1:] for s in self.in_ck + self.ds_ck if s is not None]
-        return sum(t.numel() for p in pairs for t in p) + sum(t.numel() * 4 for d in (self.sm, self.si) for t in d.values())
+        stats = sum(t.numel() * 4 for d in (self.sm, self.si) for t in d.values())
+        return sum(t.numel() for p in pairs for t in p) + stats + (self.pool_index.numel() if self.pool else 0)

@@ -5,6 +5,7 @@ import torch
 
 import oracle
 from paper_1901_09290_b200 import binding as B
+from paper_1901_09290_b200 import harness
 from paper_1901_09290_b200 import workloads as W
 from tests import helpers as Hh
 
@@ -255,3 +256,27 @@ def test_sizes_whose_products_pass_64_bits_are_refused():
             with pytest.raises(B.PtError) as e:
                 call(B.make_pack_desc(npix, 8))
             assert e.value.status == 2
+
+
+# ------------------------------------------------------------------------------------------------ the chained step
+def _network():
+    net = W.resnet50(32)
+    return W.with_sizes(net, W.uniform_keep(net, 0.2))
+
+
+def test_saved_bytes_count_what_the_backward_pass_reads():
+    """From the shapes: a code per channel, padded to 8, and a scale byte per 32 of every convolution's output, every block's input and every
+    projection; two statistics per image and group; a byte per value of the pooled stem."""
+    net, N, groups = _network(), 3, 4
+    s = harness.CheckpointedStep(Hh.ctx(), net, N, W.BASE_SEED + 7400, groups=groups, max_blocks=2)
+    ck = lambda P, K: N * P * P * W.pad8(K) + (N * P * P * ((K + 31) // 32) + 15) // 16 * 16
+    L = net.layers
+    want = sum(ck(L[i].P, L[i].K) + 2 * 4 * N * min(groups, L[i].K) for i in s.used)
+    want += sum(ck(L[m[0]].H, L[m[0]].C) for m, _, _ in s.blocks) + sum(ck(L[d].P, L[d].K) for _, d, _ in s.blocks if d is not None)
+    assert s.pool
+    want += N * s.pool_index.shape[1] ** 2 * W.pad16(L[0].K)
+    assert s.saved_bytes() == want
+    s.step()
+    torch.cuda.synchronize()
+    Hh.ctx().poll()
+    assert s.saved_bytes() == want
