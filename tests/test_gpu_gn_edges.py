@@ -280,3 +280,31 @@ def test_saved_bytes_count_what_the_backward_pass_reads():
     torch.cuda.synchronize()
     Hh.ctx().poll()
     assert s.saved_bytes() == want
+
+
+def test_group_norm_chain_is_the_same_on_side_streams():
+    """A pruned ResNet-50 chained with group norm, with the weight gradients and the projection shortcuts (their norms too, with a workspace
+    of their own) on side streams: every result is what it is on one stream, bit for bit where the launches are the same; weight gradients,
+    whose sums are split differently, to the rounding of fp32 sums over up to 200 K pixels, and bit for bit from run to run."""
+    c = Hh.ctx()
+    net, seed = W.resnet50(), W.BASE_SEED + 7500
+    netp = W.with_sizes(net, W.staged_keep_to_flops(net, seed, 0.60))
+    model = W.gen_model(netp, seed)
+    runs = []
+    for streams in (0, 2, 2):
+        s = harness.ChainedStep(c, netp, 16, seed, model=model, norm="group", wgrad_streams=streams)
+        for _ in range(2):                                       # the second step's launches meet the first one's
+            out = s.forward()
+            s.backward()
+        torch.cuda.synchronize()
+        c.poll()
+        runs.append(dict(out=[out.clone(), s.dy[0].clone()] + [t.clone() for i in s.used for t in (s.sm[i], s.si[i], s.dg[i], s.db[i])],
+                         dw=[s.dm.g[i].clone() for i in s.used]))
+        del s
+        torch.cuda.empty_cache()
+    c.set_wgrad_cta_limit(0)
+    one, a, b = runs
+    for r in (a, b):
+        assert all(torch.equal(x, y) for x, y in zip(r["out"], one["out"]))
+        assert all(float((x - y).abs().max()) <= 2e-4 * float(y.abs().max()) for x, y in zip(r["dw"], one["dw"]))
+    assert all(torch.equal(x, y) for x, y in zip(a["dw"], b["dw"]))
