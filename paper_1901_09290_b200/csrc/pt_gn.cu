@@ -115,11 +115,12 @@ __device__ __forceinline__ float rcp(float x) { float r; asm("rcp.approx.ftz.f32
 // 1e-9 at most where |z| < 2^30. A residual, which may be of the type's lowest value, is taken as -2^20 at least (a clamp of w itself took
 // 12 % longer). A NaN stays in w and leaves its neighbour in the pair alone.
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-__device__ __forceinline__ f2 sigmoid_w(f2 w)
+__device__ __forceinline__ f2 sigmoid_w(f2 w, f2 &e)                       // e: 2^w, so that 1 - sigmoid is e * sigmoid
 {
     float a, b;
     un2(w, a, b);
-    un2(add2(mk2(fminf(ex2(a), 1.152921504606846976e18f), fminf(ex2(b), 1.152921504606846976e18f)), mk2(1.f, 1.f)), a, b);
+    e = mk2(fminf(ex2(a), 1.152921504606846976e18f), fminf(ex2(b), 1.152921504606846976e18f));
+    un2(add2(e, mk2(1.f, 1.f)), a, b);
     const float r = rcp(a * b);
     return mk2(r * b, r * a);
 }
@@ -134,7 +135,10 @@ template <int ACT>
 __device__ __forceinline__ f2 activate2(f2 z)
 {
     if (ACT == PT_ACT_NONE) return z;
-    if (ACT == PT_ACT_SILU) return mul2(mul2(z, mk2(-kLn2, -kLn2)), sigmoid_w(z));       // (of w)
+    if (ACT == PT_ACT_SILU) {                                            // (of w)
+        f2 e;
+        return mul2(mul2(z, mk2(-kLn2, -kLn2)), sigmoid_w(z, e));
+    }
     float a, b;
     un2(z, a, b);
     return mk2(a > 0.f ? a : (a != a ? a : 0.f), b > 0.f ? b : (b != b ? b : 0.f));
@@ -511,9 +515,11 @@ __global__ void __launch_bounds__(kGnThreads, kGnBlocks) gn_kernel(const __grid_
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 dz[i] = from_bf(g[i]);
-                if (ACT == PT_ACT_SILU) {                                // act' = s + z*s*(1 - s) = s * (1 + w * ln 2 * (s - 1))
-                    const f2 s = sigmoid_w(z[i]);
-                    dz[i] = mul2(mul2(dz[i], s), fma2(z[i], fma2(s, mk2(kLn2, kLn2), mk2(-kLn2, -kLn2)), mk2(1.f, 1.f)));
+                if (ACT == PT_ACT_SILU) {
+                    // act' = s + z*s*(1 - s) = s * (1 - w * ln 2 * (e * s)): 1 - s by itself is a step of s wrong, and times a large z anything
+                    f2 e;
+                    const f2 s = sigmoid_w(z[i], e);
+                    dz[i] = mul2(mul2(dz[i], s), fma2(z[i], mul2(mul2(e, s), mk2(-kLn2, -kLn2)), mk2(1.f, 1.f)));
                 }
             }
         };

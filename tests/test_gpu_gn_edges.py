@@ -308,3 +308,31 @@ def test_group_norm_chain_is_the_same_on_side_streams():
         assert all(torch.equal(x, y) for x, y in zip(r["out"], one["out"]))
         assert all(float((x - y).abs().max()) <= 2e-4 * float(y.abs().max()) for x, y in zip(r["dw"], one["dw"]))
     assert all(torch.equal(x, y) for x, y in zip(a["dw"], b["dw"]))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("large", [30.0, 1e3, 1e5, 1e7, 1e12, 2.0 ** 100])
+def test_silu_gradients_at_large_values(large, packed):
+    """SiLU's slope is 1 for large z, and 0 for -z, whatever the neighbouring channels hold. dresidual: a rounding to bf16, 2^-8 of the slope, and
+    1e-5 of |dy| (what the header states for z below -41: |z| * 2^-60 at most, |z| taken as 2^20 at most)."""
+    gen = torch.Generator().manual_seed(29)
+    N, H, C, begin = 2, 7, 16, [0, 16]
+    x, dy = (W.bf16_round(torch.randn((N, H, H, C), generator=gen)) for _ in range(2))
+    r = W.bf16_round(torch.randn((N, H, H, C), generator=gen))
+    at = torch.rand((N, H, H, C), generator=gen)
+    r = torch.where(at < 0.25, W.bf16_round(torch.tensor(large)), torch.where(at < 0.4, -W.bf16_round(torch.tensor(large)), r))
+    g, b = torch.rand(C, generator=gen) + 0.5, torch.rand(C, generator=gen) - 0.5
+    mean, rstd = np.full((N, 1), 0.1, np.float32), np.full((N, 1), 1.1, np.float32)
+    dx, dres, dg, db = _backward(x, dy, g, b, mean, rstd, begin, 2, r, packed)
+    xv = oracle.act_unpack(*oracle.act_pack(x.numpy())) if packed else x.double().numpy()
+    with np.errstate(over="ignore", invalid="ignore"):
+        xhat = (xv - float(mean[0, 0])) * float(rstd[0, 0])
+        z = xhat * g.double().numpy() + b.double().numpy() + r.double().numpy()
+        e = np.exp(-np.abs(z))
+        s = np.where(z >= 0, 1.0, e) / (1.0 + e)
+        slope = s + np.where(np.abs(z) < 700, z, 0.0) * s * (np.where(z >= 0, e, 1.0) / (1.0 + e))
+    ady = np.abs(dy.double().numpy())
+    want = dy.double().numpy() * slope
+    assert np.all(np.abs(dres - want) <= 2.0 ** -8 * np.abs(want) + 1e-5 * ady)
+    assert np.all(np.abs(db - want.sum((0, 1, 2))) <= 1e-5 * 1.1 * ady.sum((0, 1, 2)))
+    assert np.all(np.abs(dg - (want * xhat).sum((0, 1, 2))) <= 1e-5 * 1.1 * (ady * np.abs(xhat)).sum((0, 1, 2)))
