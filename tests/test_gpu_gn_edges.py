@@ -1,4 +1,9 @@
 """Group norm and 8-bit checkpoints at the ends of their range, against 64-bit references. Tolerances are derived at the tests."""
+import os
+import subprocess
+import sys
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -10,6 +15,7 @@ from paper_1901_09290_b200 import workloads as W
 from tests import helpers as Hh
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 # ------------------------------------------------------------------------------------------------ checkpoints
@@ -336,3 +342,72 @@ def test_silu_gradients_at_large_values(large, packed):
     assert np.all(np.abs(dres - want) <= 2.0 ** -8 * np.abs(want) + 1e-5 * ady)
     assert np.all(np.abs(db - want.sum((0, 1, 2))) <= 1e-5 * 1.1 * ady.sum((0, 1, 2)))
     assert np.all(np.abs(dg - (want * xhat).sum((0, 1, 2))) <= 1e-5 * 1.1 * (ady * np.abs(xhat)).sum((0, 1, 2)))
+
+
+_FIRST = '''
+import torch
+from paper_1901_09290_b200 import binding as B
+c, N, H, C, G = B.Context(0), 6, 9, 24, 3
+g = torch.Generator(device="cuda").manual_seed(1)
+x, dy = (torch.randn((N, H, H, C), generator=g, device="cuda").bfloat16() for _ in range(2))
+gam, bet = torch.rand(C, device="cuda"), torch.rand(C, device="cuda")
+d, pd = B.make_gn_desc(N, H, H, C, G, act=B.PT_ACT_SILU), B.make_pack_desc(N * H * H, C)
+def bufs():
+    o = [torch.zeros((N, G), device="cuda") for _ in range(2)] + [torch.zeros_like(x) for _ in range(3)] + [torch.zeros(C, device="cuda") for _ in range(2)]
+    return o + list(B.checkpoint_buffers(N * H * H, C)) + [torch.empty(B.pt_gn_workspace_bytes(c, d), dtype=torch.uint8, device="cuda")]
+def go(mean, rstd, y, dx, back, dg, db, codes, scales, ws):
+    B.pt_gn_act_fwd(c, d, x, None, gam, bet, mean, rstd, y, codes, scales)
+    B.pt_gn_act_bwd_packed(c, d, codes, scales, None, dy, gam, bet, mean, rstd, dx, None, dg, db, None, ws)
+    B.pt_act_unpack(c, pd, codes, scales, back)
+    B.pt_act_pack(c, pd, back, codes, scales)
+a, b = bufs(), bufs()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    go(*a)
+graph.replay()
+go(*b)
+torch.cuda.synchronize()
+c.poll()
+assert all(torch.equal(p, q) for p, q in zip(a[:8], b[:8])) and a[3].abs().max() > 0
+print("same")
+'''
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    """Nothing is left to a first call that a capture does not allow."""
+    r = subprocess.run([sys.executable, "-c", _FIRST], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
+
+
+def test_two_threads_of_a_context():
+    """Calls of one context from two threads at once, on streams of their own, first ones of their shapes: as one by one."""
+    c, C, G = Hh.ctx(), 40, 5
+    gen = torch.Generator(device="cuda").manual_seed(30)
+    one, zero = torch.ones(C, device="cuda"), torch.zeros(C, device="cuda")
+    shapes = [(n, h) for n in (3, 7, 11) for h in (5, 13, 17, 23)]
+    xs = {s: torch.randn((s[0], s[1], s[1], C), generator=gen, device="cuda").bfloat16() for s in shapes}
+
+    def run(out, stream):
+        torch.cuda.set_device(0)
+        for N, H in shapes:
+            d = B.make_gn_desc(N, H, H, C, G, act=B.PT_ACT_NONE, eps=2e-5)
+            o = [torch.empty_like(xs[N, H]), torch.empty((N, G), device="cuda"), torch.empty((N, G), device="cuda")]
+            stream.wait_stream(torch.cuda.current_stream())
+            B.pt_gn_act_fwd(c, d, xs[N, H], None, one, zero, o[1], o[2], o[0], stream=stream)
+            out.append(o)
+
+    torch.cuda.synchronize()
+    outs, streams = [[], []], [torch.cuda.Stream(), torch.cuda.Stream()]
+    threads = [threading.Thread(target=run, args=a) for a in zip(outs, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    last = []
+    run(last, torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    c.poll()
+    assert len(outs[0]) == len(outs[1]) == len(shapes)
+    for a, b, e in zip(outs[0], outs[1], last):
+        assert all(torch.equal(p, r) and torch.equal(q, r) for p, q, r in zip(a, b, e))
