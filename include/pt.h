@@ -266,13 +266,15 @@ pt_status pt_bn_relu_bwd(pt_ctx *ctx, const pt_bn_desc *d, const void *x, const 
  *     A = sum(gamma*dz)/m, B = sum(gamma*dz*xhat)/m over the group, dx = rstd*(gamma*dz - A - xhat*B), dresidual = dz.
  * All pointers are device pointers but group_begin. x, residual, y, dy, dx, dresidual are 16-byte aligned [N][H][W][ld] bf16 tensors whose
  * pad lanes are never used and are written as zeros in the outputs; gamma, beta and their gradients are fp32 vectors of C elements,
- * save_mean and save_rstd fp32 [N][groups]. Sums are combined in a fixed order (run-to-run identical). An output may be the same tensor
+ * save_mean and save_rstd fp32 [N][groups]. Sums are fp32 over a thread's pixels, in 64 bits from there on in the forward pass and over many
+ * images, and combined in a fixed order (run-to-run identical). An output may be the same tensor
  * as an input of its call (y as x or residual; dx and dresidual as x, residual or dy, but not as each other); otherwise no two overlap.
  * An infinity or a NaN in x makes the outputs of its image and group NaN; a NaN in the residual stays in its element of y. The forward pass
  * wants |x| below 2^52 and var + eps above 2^-100: its squares are fp32. Where larger ones overflow, the outputs of the image and group are
  * NaN; smaller ones lose bits, and groups of equal values have no rstd where eps is 0. The backward passes take rstd from 2^-60 to 2^60.
- * PT_ACT_SILU wants
- * |gamma*xhat + beta| below 2^30 and a residual below 2^126 (it may be as low as the type goes, and leaves 0 then).
+ * PT_ACT_SILU wants |gamma*xhat + beta| below 2^30 and a residual below 2^126. Its sigmoid stays at 2^-60 where the formula's is less (z below
+ * -41.6), and a residual below -2^20 is taken as -2^20: such an element's y and slope are |z| * 2^-60 at most, which is 2^-40 behind a residual of
+ * the type's lowest value.
  * The current device must be the context's. PT_ERR_INVALID_ARG for bad sizes, pitches, alignment, groups, missing pointers or another
  * current device; PT_ERR_UNSUPPORTED for ld > 2048, more than 2^24 images, an image of 4 GB or
  * more, or more than 256 groups of unequal sizes; PT_ERR_WORKSPACE if ws is too small.

@@ -10,15 +10,18 @@
 // batches of a few pixels: there is nobody to wait for but one's own copies. A thread walks its pixels forwards for the sums; the blocks of
 // the cluster exchange the groups' sums through distributed shared memory; and it walks the pixels BACKWARDS for the results: the last
 // batches of the first walk are still in the ring, and the others were read last and are the likeliest to be in L2. Batches that the second
-// walk is done with make room for the cluster's next unit. No atomics: sums in a fixed order (run-to-run identical). Two blocks of 256
-// threads share an SM, with up to 128 registers a thread: a thread's 40 to 48 constants (five or six per channel) and two or four pixels.
+// walk is done with make room for the cluster's next unit. No atomics: sums in a fixed order (run-to-run identical). The forward pass's
+// statistics are means and squares about the mean from a thread's first few pixels on, joined in 64 bits; the backward pass's sums are fp32
+// in short chains. Two blocks of 256 threads share an SM, with up to 128 registers a thread: a thread's 40 to 48 constants (five or six per
+// channel) and two or four pixels.
 //
 // Measured (B200; in brackets the bytes that have to move, at the copy rate of 6.56 TB/s, over the time): 64x28x28x371 with ReLU and a
-// residual forward 27.4 us (0.62), backward 54.1 (0.52); 64x56x56x256 with SiLU forward 53.1 (0.59), with the checkpoint 63.0 (0.63),
-// backward 83.8 (0.56), from the checkpoint and with y again 109.5 (0.50); with ReLU 47.7, 58.8, 79.4 and 92.3. The backward pass of
-// 64x56x56x256 with SiLU reads 367 MB from DRAM where 206 would do: all images are in work at once, and the rings hold 19 of those 206 MB.
-// It issues in 53 % of the cycles, DRAM is busy in 65 %. The small ones are a row of latencies: launch, first load, sums, exchange, and
-// for the backward pass a second launch for dgamma and dbeta.
+// residual forward 27.7 us (0.61), backward 54.1 (0.52); 64x56x56x256 with SiLU forward 53.3 (0.59), with the checkpoint 63.3 (0.62),
+// backward 83.8 (0.56), from the checkpoint and with y again 110.5 (0.50); with ReLU 47.7, 59.5, 79.2 and 92.2. The backward pass of
+// 64x56x56x256 with SiLU reads 366 MB from DRAM where 206 would do: all images are in work at once, and the rings hold 19 of those 206 MB.
+// It issues in 53 % of the cycles, DRAM is busy in 63 %; both passes of 64x28x28x371 with a residual issue in 34 and 46 % and keep DRAM busy
+// in 37 and 51 %, waiting for loads and at barriers. The small ones are a row of latencies: launch, first load, sums, exchange, and for the
+// backward pass a second launch for dgamma and dbeta.
 //   (The first form had a producer warp and bulk copies of whole chunks of pixels. One thread issues such a copy every 0.3 to 0.5 us, which
 // with two or three tensors was the bound: 150 to 260 us for the backward pass at 64x28x28x371 with a residual, by the chunk's size.
 // Fewer images at a time, in rounds that fit L2, cost about 4.5 us a round and do not pay; nor do eviction hints on the copies.)
@@ -1103,9 +1106,15 @@ pt_status gn_fit(pt_ctx *c, GnKernel kernel, int index, int cl, bool two, int *n
 }
 
 // The slabs and the cluster size of the least estimated time. A unit of work costs a block about 4.5 us whatever it holds (loads, barriers,
-// exchange, all in a row), so that one unit per block is best nearly everywhere, and r per row of its threads. Microseconds by clusters of
-// 1, 2, 4, 8, 16 blocks: 183, 99, 88, 98, 126 for the backward pass at 64x56x56x256 (64 images; four slabs without clusters: 85), 48.5, 33.8,
-// 28.5, 34.4, 57.5 for the forward pass at 64x28x28x371; 92, 50, 29, 18, 13 at 2x112x112x64, and 9.4 with four slabs and 9 blocks.
+// exchange, all in a row), so that one unit per block is best nearly everywhere, and `row` per row of its threads: 0.25 to 0.55 by direction
+// and checkpoint, 0.1 more with a residual, 1.8 times that where two blocks share an SM (backward 64x56x56x256: 0.47 us a row alone, 0.85
+// together). 1.25 for slabs of less than 64 bytes a pixel, 0.7 for a cluster's exchange and 1.0 for a second block's start are guesses that
+// put close candidates in order, not measurements by themselves; bytes are not in it. Microseconds by clusters of 1, 2, 4, 8, 16 blocks:
+// 180, 97, 87, 96, 116 for the backward pass at 64x56x56x256 with SiLU (taken: four slabs without clusters, 84), 47.4, 32.6, 27.8, 36.6, 53.8
+// for the forward pass at 64x28x28x371 with a residual; 95, 51, 28, 17, 11 at 2x112x112x64 with SiLU, where four slabs and 9 blocks take
+// 8.1. Of thirteen shapes swept this way it took the best, or within 1 %, for eight, and lost 4 to 13 % at the others: 64x56x56x256 with ReLU
+// backward 79.0 (two slabs and 8 blocks 71.3), forward 48.0 (46.0); 2x112x112x64 9.0 (8.0); 128x32x32x16 forward and back from its checkpoint
+// 21.1 (clusters of two 19.9); 8x16x16x27 4.7 (4.4).
 pt_status gn_plan(pt_ctx *c, GnKernel kernel, int index, int mode, bool res, GnPlan *plan)
 {
     const bool blocks = mode == kGnFwdPack || mode == kGnBwdPacked;
